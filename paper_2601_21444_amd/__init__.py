@@ -23,3 +23,13 @@ from .binding import (  # noqa: F401
     status_string,
     tensor_view,
 )
+from .cache import (  # noqa: F401
+    ApbvCache,
+    CACHE_MAX_REQUESTS,
+    apbv_cache_attention,
+    apbv_cache_attention_workspace_bytes,
+    apbv_cache_empty,
+    apbv_cache_load,
+    apbv_cache_map,
+    apbv_cache_store,
+)

@@ -55,6 +55,17 @@ class ApbvAttentionItem(ctypes.Structure):
     ]
 
 
+class ApbvCacheStruct(ctypes.Structure):
+    """Mirror of ``apbv_cache`` in include/apbv_cache.h."""
+    _fields_ = [
+        ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+        ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+        ("n_pages", ctypes.c_int64),
+        ("page_stride_codes", ctypes.c_int64), ("page_stride_scales", ctypes.c_int64),
+        ("page_size", ctypes.c_int32),
+    ]
+
+
 class _NoMarshal:
     """In place of the native marshalling where there is none: no call is the plain one."""
 
@@ -134,6 +145,26 @@ def load_library() -> ctypes.CDLL:
     lib.apbv_host_attention_group.argtypes = [
         ctypes.c_int, ctypes.POINTER(ApbvAttentionItem), ctypes.c_int, ctypes.c_int, ctypes.c_int,
         ctypes.c_float, ctypes.c_void_p]
+    lib.apbv_cache_map.restype = ctypes.c_int
+    lib.apbv_cache_map.argtypes = [
+        ctypes.c_int, ctypes.c_int, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+        ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+    lib.apbv_cache_store.restype = ctypes.c_int
+    lib.apbv_cache_store.argtypes = [
+        ctypes.POINTER(ApbvCacheStruct), ctypes.c_int, ctypes.c_int, ApbvTensor, ApbvTensor, ctypes.c_void_p, ctypes.c_void_p]
+    lib.apbv_cache_load.restype = ctypes.c_int
+    lib.apbv_cache_load.argtypes = [
+        ctypes.POINTER(ApbvCacheStruct), ctypes.c_int, ctypes.c_int, ctypes.c_int64,
+        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+    lib.apbv_cache_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.apbv_cache_attention_workspace_bytes.argtypes = [
+        ctypes.c_int, ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int64]
+    lib.apbv_cache_attention.restype = ctypes.c_int
+    lib.apbv_cache_attention.argtypes = [
+        ctypes.POINTER(ApbvCacheStruct), ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ApbvTensor,
+        ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int,
+        ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
     _native = _load_marshal(lib)
     _lib = lib
     return lib

@@ -22,6 +22,9 @@ MARSHAL = os.path.join(PKG, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = {
     "api.hip": [],
     "attention.hip": ["-fno-honor-nans"],
+    "cache.hip": [],
+    "cache_api.hip": [],
+    "cache_attention.hip": ["-fno-honor-nans"],
     "compress.hip": [],
     "merge.hip": [],
     "packed_attention.hip": ["-fno-honor-nans"],

@@ -1,0 +1,129 @@
+// Host-side argument validation and planning of the cache's C ABI (include/apbv_cache.h); plain C++ as host_validation.h is.
+#pragma once
+#include "apbv_cache.h"
+#include "host_validation.h"
+
+namespace apbv {
+
+constexpr int64_t kMaxSlots = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxCachedTokens = (int64_t)1 << 30;      // of one request
+constexpr int kCacheBlock = 32;             // elements that share a scale
+
+inline bool valid_page_size(int p) { return p == 16 || p == 32 || p == 64 || p == 128 || p == 256; }
+inline int log2_page(int p) { return p == 16 ? 4 : p == 32 ? 5 : p == 64 ? 6 : p == 128 ? 7 : 8; }
+
+inline apbv_status check_cache(const apbv_cache* c, int hkv, int d) {
+  if (c == nullptr) return APBV_ERR_NULL;
+  if (hkv < 1 || hkv > 65535) return APBV_ERR_SHAPE;
+  if (d != 64 && d != 128) return APBV_ERR_UNSUPPORTED;
+  if (!valid_page_size(c->page_size)) return APBV_ERR_UNSUPPORTED;
+  if (c->n_pages < 1 || c->n_pages > kMaxSlots / c->page_size) return APBV_ERR_SHAPE;
+  if (c->k_codes == nullptr || c->v_codes == nullptr || c->k_scales == nullptr || c->v_scales == nullptr) return APBV_ERR_NULL;
+  for (const void* p : {c->k_codes, c->v_codes, c->k_scales, c->v_scales})
+    if (!aligned(p, 16)) return APBV_ERR_SHAPE;
+  const int64_t rows = (int64_t)hkv * c->page_size;
+  if (c->page_stride_codes % 16 || c->page_stride_scales % 16) return APBV_ERR_SHAPE;
+  if (c->n_pages > 1 && (c->page_stride_codes < rows * (d / 2) || c->page_stride_scales < rows * (d / kCacheBlock))) return APBV_ERR_SHAPE;
+  // (a page's bytes are kept in 32 bits; pages lie within 2^62 bytes of the first)
+  if (rows * (d / 2) > ((int64_t)1 << 30) || c->page_stride_codes >= (int64_t)1 << 31 || c->page_stride_scales >= (int64_t)1 << 31) return APBV_ERR_UNSUPPORTED;
+  return APBV_OK;
+}
+
+// A table of max_blocks entries a request.
+inline apbv_status check_table(int n_requests, int page_size, const void* table, int64_t stride, int64_t max_blocks) {
+  if (n_requests < 1) return APBV_ERR_SHAPE;
+  if (n_requests > APBV_CACHE_MAX_REQUESTS) return APBV_ERR_UNSUPPORTED;
+  if (max_blocks < 1 || max_blocks > kMaxCachedTokens / page_size) return APBV_ERR_SHAPE;
+  if (table == nullptr) return APBV_ERR_NULL;
+  if (!aligned(table, 4)) return APBV_ERR_SHAPE;
+  if (n_requests > 1 && stride < max_blocks) return APBV_ERR_SHAPE;
+  return APBV_OK;
+}
+
+inline apbv_status validate_cache_map(int n_requests, int page_size, int64_t max_blocks, const int32_t* old_lengths,
+                                      const int32_t* new_lengths, const int32_t* table, int64_t table_stride, const int32_t* free_pages,
+                                      int64_t free_capacity, const int32_t* free_count, int64_t max_new_tokens, const int32_t* lengths_out,
+                                      const int32_t* starts_out, const int32_t* slots_out, const int32_t* free_count_out) {
+  if (!valid_page_size(page_size)) return APBV_ERR_UNSUPPORTED;
+  const apbv_status st = check_table(n_requests, page_size, table, table_stride, max_blocks);
+  if (st != APBV_OK) return st;
+  if (free_capacity < 0 || free_capacity > kMaxSlots || max_new_tokens < 0 || max_new_tokens > kMaxTokens) return APBV_ERR_SHAPE;
+  if (old_lengths == nullptr || new_lengths == nullptr || free_count == nullptr || lengths_out == nullptr || starts_out == nullptr ||
+      free_count_out == nullptr || (free_pages == nullptr && free_capacity > 0) || (slots_out == nullptr && max_new_tokens > 0))
+    return APBV_ERR_NULL;
+  for (const void* p : {old_lengths, new_lengths, free_pages, free_count, lengths_out, starts_out, slots_out, free_count_out})
+    if (!aligned(p, 4)) return APBV_ERR_SHAPE;
+  if (lengths_out == new_lengths) return APBV_ERR_SHAPE;
+  return APBV_OK;
+}
+
+inline apbv_status validate_cache_store(const apbv_cache* cache, int hkv, int d, const apbv_tensor& k, const apbv_tensor& v, const int32_t* slots) {
+  apbv_status st = check_cache(cache, hkv, d);
+  if (st != APBV_OK) return st;
+  if ((st = check_view(k, hkv, d, 1, true)) != APBV_OK) return st;
+  if ((st = check_view(v, hkv, d, 1, true)) != APBV_OK) return st;
+  if (k.tokens != v.tokens) return APBV_ERR_SHAPE;
+  if (k.tokens > 0 && slots == nullptr) return APBV_ERR_NULL;
+  if (!aligned(slots, 4)) return APBV_ERR_SHAPE;
+  return APBV_OK;
+}
+
+inline apbv_status validate_cache_load(const apbv_cache* cache, int hkv, int d, int64_t tokens, const int32_t* slots, const void* k_out,
+                                       const void* v_out) {
+  const apbv_status st = check_cache(cache, hkv, d);
+  if (st != APBV_OK) return st;
+  if (tokens < 0 || tokens > kMaxTokens) return APBV_ERR_SHAPE;
+  if (tokens > 0 && (slots == nullptr || k_out == nullptr || v_out == nullptr)) return APBV_ERR_NULL;
+  if (!aligned(slots, 4) || !aligned(k_out, 16) || !aligned(v_out, 16)) return APBV_ERR_SHAPE;
+  return APBV_OK;
+}
+
+inline apbv_status validate_cache_attention(const apbv_cache* cache, int n_requests, int hq, int hkv, int d, const apbv_tensor& q,
+                                            const int32_t* table, int64_t table_stride, int64_t max_blocks, const int32_t* lengths,
+                                            const int32_t* q_starts, int64_t max_q, float softmax_scale, const void* out,
+                                            const float* lse_out) {
+  apbv_status st = check_heads(1, hq, hkv, d);
+  if (st != APBV_OK) return st;
+  if ((st = check_cache(cache, hkv, d)) != APBV_OK) return st;
+  if ((st = check_table(n_requests, cache->page_size, table, table_stride, max_blocks)) != APBV_OK) return st;
+  if ((st = check_view(q, hq, d, 1, true)) != APBV_OK) return st;
+  if (lengths == nullptr) return APBV_ERR_NULL;
+  if (!aligned(lengths, 4) || !aligned(q_starts, 4)) return APBV_ERR_SHAPE;
+  if (q_starts == nullptr && q.tokens % n_requests) return APBV_ERR_SHAPE;
+  if (q.tokens * (hq / hkv) > (int64_t)1 << 30) return APBV_ERR_UNSUPPORTED;      // rows of a KV head: kept in 32 bits
+  if (max_q < 0 || max_q > kMaxTokens) return APBV_ERR_SHAPE;
+  if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale)) return APBV_ERR_SHAPE;
+  if (q.tokens > 0 && out == nullptr) return APBV_ERR_NULL;
+  if (!aligned(out, 16) || !aligned(lse_out, 4)) return APBV_ERR_SHAPE;
+  return APBV_OK;
+}
+
+// ---- how an attention call is cut.  The keys of all requests, KV heads and row tiles are one axis of 64-key tiles (the
+// device knows its length, the host does not), dealt to `workgroups` equal shares; a share that begins or ends inside a
+// (request, head, row tile) leaves a part of it in the workspace: at most two a workgroup.
+constexpr int kCacheKeyTile = 64;
+struct CachePlan {
+  int rows;          // query rows (query x head of the KV group) of a row tile
+  int workgroups;
+  int least_tiles;   // a share is not shorter than this
+};
+inline CachePlan choose_cache_plan(int n_requests, int64_t n_rows, int hq, int hkv, int64_t max_q) {
+  (void)n_requests;
+  (void)n_rows;
+  const int64_t rows = max_q * (hq / hkv);
+  CachePlan p;
+  p.rows = rows <= 16 ? 16 : 32;
+  p.workgroups = 512;
+  p.least_tiles = 4;
+  return p;
+}
+inline size_t cache_part_bytes(int rows, int d) { return (size_t)rows * (size_t)(d + 2) * sizeof(float); }
+inline size_t cache_attention_workspace_bytes(int n_requests, int64_t n_rows, int hq, int hkv, int d, int64_t max_q) {
+  if (check_heads(1, hq, hkv, d) != APBV_OK || n_requests < 1 || n_requests > APBV_CACHE_MAX_REQUESTS || n_rows < 0 || n_rows > kMaxTokens ||
+      n_rows * (hq / hkv) > (int64_t)1 << 30 || max_q < 0 || max_q > kMaxTokens)
+    return 0;
+  const CachePlan p = choose_cache_plan(n_requests, n_rows, hq, hkv, max_q);
+  return align256((size_t)p.workgroups * 2 * cache_part_bytes(p.rows, d));
+}
+
+}  // namespace apbv
