@@ -102,6 +102,8 @@ inline apbv_status validate_cache_attention(const apbv_cache* cache, int n_reque
 // device knows its length, the host does not), dealt to `workgroups` equal shares; a share that begins or ends inside a
 // (request, head, row tile) leaves a part of it in the workspace: at most two a workgroup.
 constexpr int kCacheKeyTile = 64;
+constexpr int kCacheWaves = 4;              // waves of a workgroup
+constexpr int kCacheJoinRows = 512;         // rows (query x head) up to which several waves join the parts of one
 struct CachePlan {
   int rows;          // query rows (query x head of the KV group) of a row tile
   int workgroups;
@@ -123,7 +125,8 @@ inline size_t cache_attention_workspace_bytes(int n_requests, int64_t n_rows, in
       n_rows * (hq / hkv) > (int64_t)1 << 30 || max_q < 0 || max_q > kMaxTokens)
     return 0;
   const CachePlan p = choose_cache_plan(n_requests, n_rows, hq, hkv, max_q);
-  return align256((size_t)p.workgroups * 2 * cache_part_bytes(p.rows, d));
+  const size_t heads = p.rows == 16 ? 0 : (size_t)kCacheWaves * p.rows * d * sizeof(float);      // pieces that have no room in LDS
+  return align256((size_t)p.workgroups * (2 * cache_part_bytes(p.rows, d) + heads));
 }
 
 }  // namespace apbv
