@@ -116,7 +116,8 @@ size_t apbv_cache_attention_workspace_bytes(int n_requests, int64_t n_rows, int 
  * rounded to bf16.  How the keys are cut depends on the shape of the call and on all lengths; results of the same call are
  * repeatable.
  * Supported: head_dim in {64, 128}; n_q_heads % n_kv_heads == 0; 1 <= n_requests <= 4096; max_blocks * page_size <= 2^30;
- * n_rows * G <= 2^30.
+ * n_rows * G <= 2^30; (n_rows * G / 16 + n_requests) * n_kv_heads * (max_blocks * page_size / 64) below 2^31 (a table of
+ * 4096 rows for 2^20 tokens, with 8 KV heads).
  */
 apbv_status apbv_cache_attention(const apbv_cache* cache, int n_requests, int n_q_heads, int n_kv_heads, int head_dim,
                                  apbv_tensor q, const int32_t* block_table, int64_t table_stride, int64_t max_blocks,

@@ -25,6 +25,7 @@ SOURCES = {
     "cache.hip": [],
     "cache_api.hip": [],
     "cache_attention.hip": ["-fno-honor-nans"],
+    "cache_block_attention.hip": ["-fno-honor-nans"],
     "compress.hip": [],
     "merge.hip": [],
     "packed_attention.hip": ["-fno-honor-nans"],

@@ -55,9 +55,10 @@ struct CacheAttnParams {
   int n_requests, n_rows, each;     // each: rows of every request where starts is nullptr
   int max_len;             // the longest length a row of the table holds
   int hq, hkv, group, causal;
-  int workgroups, least_tiles;
+  int workgroups, short_tiles, least_tiles;
   float scale_log2;        // softmax_scale * log2(e)
 };
+apbv_status launch_cache_block_attention(const CacheAttnParams& p, int head_dim, hipStream_t stream);      // the parts are left to join
 apbv_status launch_cache_attention(const CacheAttnParams& p, const CachePlan& plan, int head_dim, hipStream_t stream);
 
 }  // namespace apbv

@@ -15,212 +15,12 @@
 // is free as long as K and Q agree: lane (key li, quarter lg) takes the quarter's 16 bytes of codes, one load, all of one
 // scale block, and converts eight of them a k-step.  No LDS.  V is needed transposed: a lane converts its quarter of a key's
 // row, writes it to the wave's own LDS tile as bf16, and the transposing LDS read does the rest.
-#include "attention_tiles.h"
-#include "cache.h"
+#include "cache_tiles.h"
 
 namespace apbv {
 namespace {
 
-#define APBV_CONST(T) const __attribute__((address_space(4))) T*     // read through the scalar cache
-__device__ __forceinline__ int scalar_load(const int32_t* p, int64_t i) { return ((APBV_CONST(int32_t))p)[i]; }
-
-struct Request {
-  int first, rows, len;      // first query, rows (query x head of the group), keys
-  int tiles;                 // 64-key tiles of each of its row tiles; 0: none
-};
-
-__device__ __forceinline__ int clip(int x, int hi) { return x < 0 ? 0 : (x > hi ? hi : x); }
-__device__ __forceinline__ Request request_of(const CacheAttnParams& p, int first, int past, int len) {
-  Request r;
-  r.first = clip(first, p.n_rows);
-  past = clip(past, p.n_rows);
-  r.rows = (past > r.first ? past - r.first : 0) * p.group;
-  r.len = clip(len, p.max_len);
-  r.tiles = r.rows > 0 ? (r.len + kCacheKeyTile - 1) / kCacheKeyTile : 0;
-  return r;
-}
-__device__ __forceinline__ int64_t readlane64(int64_t x, int lane) {
-  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, lane), hi = __builtin_amdgcn_readlane((uint32_t)((uint64_t)x >> 32), lane);
-  return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
-// x / y for 0 <= x, 0 < y; almost always within 32 bits, where it takes a fifth of the instructions.
-__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
-  if (((uint64_t)x | (uint64_t)y) >> 32 == 0) return (int64_t)((uint32_t)x / (uint32_t)y);
-  return x / y;
-}
-
-// Inclusive sums over the lanes of a wave, on the DPP path.
-template <int kCtrl, int kRows>
-__device__ __forceinline__ int64_t dpp64(int64_t x) {
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, kCtrl, kRows, 0xf, false);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)((uint64_t)x >> 32), kCtrl, kRows, 0xf, false);
-  return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-__device__ __forceinline__ int64_t wave_scan(int64_t x) {
-  x += dpp64<0x111, 0xf>(x);      // row_shr 1, 2, 4, 8: within sixteen lanes
-  x += dpp64<0x112, 0xf>(x);
-  x += dpp64<0x114, 0xf>(x);
-  x += dpp64<0x118, 0xf>(x);
-  x += dpp64<0x142, 0xa>(x);      // row_bcast 15: lane 15 to the second sixteen, lane 47 to the fourth
-  x += dpp64<0x143, 0xc>(x);      // row_bcast 31: lane 31 to the upper half
-  return x;
-}
-
-// The axis of tiles: its length, and where the requests lie on it.  A wave holds a window of 64 consecutive requests, one a
-// lane, handed from lane to lane as they are needed; with more than 64 it first adds up 64 groups of `per` (at most 64).
-template <int R>
-struct Axis {
-  int64_t total;
-  int base;                  // the window: request base + lane is `mine`
-  int64_t base_begin;        // where the window begins on the axis
-  Request mine;
-  int64_t past;              // where `mine` ends
-  int per, group_first;      // this lane's group: its first query row ...
-  int64_t group_past;        // ... and where it ends
-
-  __device__ __forceinline__ static int64_t tiles(const CacheAttnParams& p, const Request& r) {
-    return (int64_t)((r.rows + R - 1) / R) * p.hkv * r.tiles;
-  }
-  __device__ __forceinline__ static Request load(const CacheAttnParams& p, int b) {
-    const int first = p.starts ? p.starts[b] : b * p.each, past_row = p.starts ? p.starts[b + 1] : (b + 1) * p.each;
-    return request_of(p, first, past_row, p.lengths[b]);
-  }
-  __device__ __forceinline__ void window(const CacheAttnParams& p, int from, int64_t begin) {
-    base = from;
-    base_begin = begin;
-    mine = Request{0x7fffffff, 0, 0, 0};
-    const int b = from + (int)(threadIdx.x & 63);
-    if (b < p.n_requests) mine = load(p, b);
-    past = begin + wave_scan(tiles(p, mine));
-  }
-  __device__ __forceinline__ Axis(const CacheAttnParams& p) {
-    if (p.n_requests <= 64) {
-      window(p, 0, 0);
-      total = readlane64(past, 63);
-      return;
-    }
-    const int lane = threadIdx.x & 63;
-    per = (p.n_requests + 63) / 64;
-    group_first = 0x7fffffff;
-    int64_t sum = 0;
-    for (int u = 0; u < per; u += 4) {
-      Request r[4];
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {                        // (four at a time on their way)
-        const int b = lane * per + u + v;
-        r[v] = load(p, b < p.n_requests ? b : p.n_requests - 1);
-        if (u + v >= per || b >= p.n_requests) r[v].rows = 0;
-        else if (u + v == 0) group_first = r[v].first;
-      }
-#pragma unroll
-      for (int v = 0; v < 4; ++v) sum += tiles(p, r[v]);
-    }
-    group_past = wave_scan(sum);
-    total = readlane64(group_past, 63);
-  }
-  __device__ __forceinline__ void group_window(const CacheAttnParams& p, int group) {
-    window(p, group * per, group > 0 ? readlane64(group_past, group - 1) : 0);
-  }
-  __device__ __forceinline__ int64_t begin_of(int b) const {                   // b of the window
-    return b > base ? readlane64(past, b - base - 1) : base_begin;
-  }
-  __device__ __forceinline__ Request at(const CacheAttnParams& p, int b) {     // b uniform
-    if ((unsigned)(b - base) >= 64u) window(p, b, 0);      // (a walk that leaves the window knows where it is)
-    Request r;
-    r.first = __builtin_amdgcn_readlane(mine.first, b - base);
-    r.rows = __builtin_amdgcn_readlane(mine.rows, b - base);
-    r.len = __builtin_amdgcn_readlane(mine.len, b - base);
-    r.tiles = __builtin_amdgcn_readlane(mine.tiles, b - base);
-    return r;
-  }
-  // Length of a workgroup's share.
-  __device__ __forceinline__ int64_t share(const CacheAttnParams& p) const {
-    const int64_t q = quotient(total + p.workgroups - 1, p.workgroups);
-    return q > p.least_tiles ? q : p.least_tiles;
-  }
-  // The request that holds tile `pos` < total.
-  __device__ __forceinline__ int find(const CacheAttnParams& p, int64_t pos) {
-    if (p.n_requests > 64) group_window(p, __builtin_ctzll(__builtin_amdgcn_ballot_w64(group_past > pos)));
-    return base + __builtin_ctzll(__builtin_amdgcn_ballot_w64(past > pos));
-  }
-  // The last request that begins at or before this query row (the first one if there is none).
-  __device__ __forceinline__ int find_row(const CacheAttnParams& p, int row) {
-    if (p.n_requests > 64) {
-      const uint64_t before = __builtin_amdgcn_ballot_w64(group_first <= row);
-      group_window(p, before ? 63 - __builtin_clzll(before) : 0);
-    }
-    const uint64_t before = __builtin_amdgcn_ballot_w64(mine.first <= row);
-    return base + (before ? 63 - __builtin_clzll(before) : 0);
-  }
-};
-
 enum : int { kHead = 1, kTail = 2, kSpan = 4 };            // what a wave keeps of row tiles that are not its own alone
-
-// A 16-key block's codes (16 bytes a lane at head_dim 128, 8 at 64) and scale byte.
-template <int D>
-struct Codes {
-  static constexpr int kWords = D / 32;
-  uint32_t w[kWords];
-  uint32_t scale;
-  // uniform bases, and how far behind them the block lies; this lane's key li of it, quarter lg
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int code_step, int scale_step, int li, int lg) {
-    if constexpr (D == 128) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(codes + (uint32_t)(li * 64 + lg * 16) + code_step);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = x[i];
-      scale = scales[(uint32_t)(li * 4 + lg) + scale_step];
-    } else {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(codes + (uint32_t)(li * 32 + lg * 8) + code_step);
-      w[0] = x[0];
-      w[1] = x[1];
-      scale = scales[(uint32_t)(li * 2 + (lg >> 1)) + scale_step];
-    }
-  }
-  // eight elements as bf16
-  __device__ __forceinline__ u32x4 values(int i) const {
-    const float s = __uint_as_float(scale << 23);
-    u32x4 x;
-    x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 0));
-    x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 1));
-    x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 2));
-    x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 3));
-    return x;
-  }
-};
-
-// Where the four 16-key blocks of a tile lie (uniform), as byte offsets into the codes and the scales of K and of V, and which
-// blocks are not there.  A page of 64 tokens or more holds a whole tile: one lookup, and the blocks follow one another.
-template <int D, bool kOnePage>
-struct Blocks {
-  static constexpr int kLookups = kOnePage ? 1 : 4;
-  int64_t codes[kLookups], scales[kLookups];
-  int absent;                // bit i: the page of lookup i is out of range, or no key of the request lies in it
-  __device__ __forceinline__ void find(const CacheAttnParams& p, const int32_t* table_row, int head, int len, int tile) {
-    absent = 0;
-#pragma unroll
-    for (int i = 0; i < kLookups; ++i) {
-      const int token = tile * kCacheKeyTile + 16 * i;
-      const int at = token < len ? token : len - 1;                      // (a table entry that the request has)
-      const int page = scalar_load(table_row, at >> p.cache.page_log2);
-      const bool there = token < len && (unsigned)page < (unsigned)p.cache.n_pages;
-      absent |= there ? 0 : 1 << i;
-      const int pg = there ? page : 0;
-      const int row = (head << p.cache.page_log2) + (token & ((1 << p.cache.page_log2) - 1));
-      codes[i] = (int64_t)((uint64_t)(uint32_t)pg * (uint32_t)p.cache.stride_codes) + (uint32_t)row * (uint32_t)(D / 2);
-      scales[i] = (int64_t)((uint64_t)(uint32_t)pg * (uint32_t)p.cache.stride_scales) + (uint32_t)row * (uint32_t)(D / 32);
-    }
-  }
-  __device__ __forceinline__ bool gone(int kb) const { return (absent >> (kOnePage ? 0 : kb) & 1) != 0; }
-  // this lane's pieces of the four blocks of K or of V
-  __device__ __forceinline__ void load(Codes<D> (&x)[4], const uint8_t* code_base, const uint8_t* scale_base, int li, int lg) const {
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-      constexpr int kCodeStep = kOnePage ? 16 * (D / 2) : 0, kScaleStep = kOnePage ? 16 * (D / 32) : 0;
-      x[kb].load(code_base + codes[kOnePage ? 0 : kb], scale_base + scales[kOnePage ? 0 : kb], kb * kCodeStep, kb * kScaleStep, li, lg);
-    }
-  }
-};
 
 template <int D, int NQ, bool kOnePage>
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(const CacheAttnParams p) {
@@ -238,16 +38,15 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int li = lane & 15, lg = lane >> 4;
   Axis<R> axis(p);
-  const int64_t share = axis.share(p);
-  // consecutive shares on one XCD: row tiles of a head read the same keys
-  const int wg = p.workgroups % kXcds == 0 ? (int)(blockIdx.x % kXcds) * (p.workgroups / kXcds) + (int)(blockIdx.x / kXcds) : (int)blockIdx.x;
-  const int64_t wg_begin = wg * share;
-  const int64_t wg_end = wg_begin + share < axis.total ? wg_begin + share : axis.total;
-  if (wg_begin >= wg_end) return;
+  const uint32_t share = axis.share(p);
+  const int wg = axis.my_share(share);
+  if (wg < 0) return;
+  const uint32_t wg_begin = wg * share;
+  const uint32_t wg_end = share < axis.total - wg_begin ? wg_begin + share : axis.total;
   // a wave's part of the share
-  const int64_t wave_share = (wg_end - wg_begin + W - 1) / W;
-  int64_t pos = wg_begin + wave * wave_share;
-  const int64_t end = pos + wave_share < wg_end ? pos + wave_share : wg_end;
+  const uint32_t wave_share = (wg_end - wg_begin + W - 1) / W;
+  uint32_t pos = wg_begin + wave * wave_share;
+  const uint32_t end = pos + wave_share < wg_end ? pos + wave_share : wg_end;
   int keeps = 0;
 
   // per-lane LDS offsets: V rows as written, and as the A operand of O^T (query_attention.hip)
@@ -266,7 +65,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
   const float inv_scale_log2 = 1.0f / p.scale_log2;
 
   int b = 0;
-  int64_t begin = 0;
+  uint32_t begin = 0;
   if (pos < end) {
     b = axis.find(p, pos);
     begin = axis.begin_of(b);
@@ -275,17 +74,16 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
   while (pos < end) {
     const Request rq = axis.at(p, b);
     const int row_tiles = (rq.rows + R - 1) / R;
-    const int64_t of_request = (int64_t)row_tiles * p.hkv * rq.tiles;
+    const uint32_t of_request = (uint32_t)(row_tiles * p.hkv) * (uint32_t)rq.tiles;
     if (pos >= begin + of_request) {                       // (or a request with nothing to do)
       begin += of_request;
       ++b;
       continue;
     }
-    const int64_t rel = pos - begin;
-    const int64_t item = quotient(rel, rq.tiles);
-    const int head = (int)quotient(item, row_tiles), rt = (int)(item - (int64_t)head * row_tiles);
-    const int t0 = (int)(rel - item * rq.tiles);
-    const int t1 = end - pos < rq.tiles - t0 ? t0 + (int)(end - pos) : rq.tiles;
+    const uint32_t rel = pos - begin, item = rel / (uint32_t)rq.tiles;
+    const int head = (int)(item / (uint32_t)row_tiles), rt = (int)(item - (uint32_t)head * row_tiles);
+    const int t0 = (int)(rel - item * (uint32_t)rq.tiles);
+    const int t1 = end - pos < (uint32_t)(rq.tiles - t0) ? t0 + (int)(end - pos) : rq.tiles;
     pos += t1 - t0;
 
     // ---- the row tile's rows: keys each sees, and Q^T fragments (k-step c of lane lg: elements lg * D / 4 + 8 c ...)
@@ -346,6 +144,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
 
       // ---- hidden keys: out of sight of a row, or not there at all, whose values may be anything
       if ((t + 1) * kCacheKeyTile > all || now.absent != 0) {
+        asm volatile("" ::: "memory");                     // (a branch, not selects in every tile)
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
           const int j = t * kCacheKeyTile + 16 * kb;
@@ -616,10 +415,12 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
   if (rq.tiles > 0) {
-    const int64_t share = axis.share(p);
+    const uint32_t share = axis.share(p);
     const int r = i * p.group + h % p.group, rt = r / R, row_tiles = (rq.rows + R - 1) / R;
-    const int64_t from = axis.begin_of(b) + ((int64_t)(h / p.group) * row_tiles + rt) * rq.tiles;
-    const int first = (int)quotient(from, share), last = (int)quotient(from + rq.tiles - 1, share);
+    const uint32_t from = axis.begin_of(b) + (uint32_t)(h / p.group * row_tiles + rt) * (uint32_t)rq.tiles;
+    const int first = (int)(from / share);
+    int last = (int)((from + rq.tiles - 1) / share);
+    last = last < p.workgroups ? last : p.workgroups - 1;
     if (first == last) return;                             // written by its only workgroup
     const float* stat = p.parts + (int64_t)p.workgroups * 2 * (R * D) + (int64_t)(r % R) * p.workgroups;
     const float* rows = p.parts + (r % R) * D + 4 * c;
@@ -687,28 +488,37 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
   if (p.lse != nullptr && lane == 0) p.lse[(int64_t)h * p.n_rows + row] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-template <int D, int NQ, bool kOnePage>
-apbv_status launch_variant(const CacheAttnParams& p, hipStream_t stream) {
+template <int D, int R>
+void launch_join(Launcher& launch, const CacheAttnParams& p) {
   const int64_t rows = (int64_t)p.n_rows * p.hq;
-  if (rows > 0x7fffffff) return APBV_ERR_UNSUPPORTED;
-  Launcher launch(stream);
-  launch(cache_attention_kernel<D, NQ, kOnePage>, dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
   if (rows <= kCacheJoinRows)
-    launch(cache_join_kernel<D, 16 * NQ, 16>, dim3((unsigned)rows), dim3(1024), 0, p);
+    launch(cache_join_kernel<D, R, 16>, dim3((unsigned)rows), dim3(1024), 0, p);
   else
-    launch(cache_join_kernel<D, 16 * NQ, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, p);
-  return launch.status();
+    launch(cache_join_kernel<D, R, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, p);
 }
-template <int D, int NQ>
-apbv_status launch_rows(const CacheAttnParams& p, hipStream_t stream) {
-  return (1 << p.cache.page_log2) >= kCacheKeyTile ? launch_variant<D, NQ, true>(p, stream) : launch_variant<D, NQ, false>(p, stream);
+template <int D>
+apbv_status launch_dim(const CacheAttnParams& p, int rows, hipStream_t stream) {
+  if ((int64_t)p.n_rows * p.hq > 0x7fffffff) return APBV_ERR_UNSUPPORTED;
+  Launcher launch(stream);
+  const bool one_page = (1 << p.cache.page_log2) >= kCacheKeyTile;
+  if (rows == kCacheBlockRows) {
+    const apbv_status st = launch_cache_block_attention(p, D, stream);
+    if (st != APBV_OK) return st;
+    launch_join<D, kCacheBlockRows>(launch, p);
+  } else if (rows == 32) {
+    launch(one_page ? cache_attention_kernel<D, 2, true> : cache_attention_kernel<D, 2, false>, dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
+    launch_join<D, 32>(launch, p);
+  } else {
+    launch(one_page ? cache_attention_kernel<D, 1, true> : cache_attention_kernel<D, 1, false>, dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
+    launch_join<D, 16>(launch, p);
+  }
+  return launch.status();
 }
 
 }  // namespace
 
 apbv_status launch_cache_attention(const CacheAttnParams& p, const CachePlan& plan, int head_dim, hipStream_t stream) {
-  if (head_dim == 128) return plan.rows == 16 ? launch_rows<128, 1>(p, stream) : launch_rows<128, 2>(p, stream);
-  return plan.rows == 16 ? launch_rows<64, 1>(p, stream) : launch_rows<64, 2>(p, stream);
+  return head_dim == 128 ? launch_dim<128>(p, plan.rows, stream) : launch_dim<64>(p, plan.rows, stream);
 }
 
 }  // namespace apbv

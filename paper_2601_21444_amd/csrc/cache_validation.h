@@ -78,6 +78,13 @@ inline apbv_status validate_cache_load(const apbv_cache* cache, int hkv, int d, 
   return APBV_OK;
 }
 
+// The tiles of all (request, KV head, row tile) are numbered in 32 bits; the host knows the most there can be.
+constexpr int kCacheKeyTile = 64;
+inline bool cache_axis_fits(int64_t n_requests, int64_t n_rows, int hq, int hkv, int64_t max_len) {
+  const int64_t row_tiles = (n_rows * (hq / hkv) / 16 + n_requests) * hkv;               // below 2^27 * 2^16
+  return row_tiles <= (int64_t)0x7fff0000 / ((max_len + kCacheKeyTile - 1) / kCacheKeyTile);
+}
+
 inline apbv_status validate_cache_attention(const apbv_cache* cache, int n_requests, int hq, int hkv, int d, const apbv_tensor& q,
                                             const int32_t* table, int64_t table_stride, int64_t max_blocks, const int32_t* lengths,
                                             const int32_t* q_starts, int64_t max_q, float softmax_scale, const void* out,
@@ -87,6 +94,7 @@ inline apbv_status validate_cache_attention(const apbv_cache* cache, int n_reque
   if ((st = check_cache(cache, hkv, d)) != APBV_OK) return st;
   if ((st = check_table(n_requests, cache->page_size, table, table_stride, max_blocks)) != APBV_OK) return st;
   if ((st = check_view(q, hq, d, 1, true)) != APBV_OK) return st;
+  if (!cache_axis_fits(n_requests, q.tokens, hq, hkv, max_blocks * cache->page_size)) return APBV_ERR_UNSUPPORTED;
   if (lengths == nullptr) return APBV_ERR_NULL;
   if (!aligned(lengths, 4) || !aligned(q_starts, 4)) return APBV_ERR_SHAPE;
   if (q_starts == nullptr && q.tokens % n_requests) return APBV_ERR_SHAPE;
@@ -101,22 +109,27 @@ inline apbv_status validate_cache_attention(const apbv_cache* cache, int n_reque
 // ---- how an attention call is cut.  The keys of all requests, KV heads and row tiles are one axis of 64-key tiles (the
 // device knows its length, the host does not), dealt to `workgroups` equal shares; a share that begins or ends inside a
 // (request, head, row tile) leaves a part of it in the workspace: at most two a workgroup.
-constexpr int kCacheKeyTile = 64;
+constexpr int kCacheBlockRows = 128;        // rows of a row tile of query blocks and chunks
 constexpr int kCacheWaves = 4;              // waves of a workgroup
 constexpr int kCacheJoinRows = 512;         // rows (query x head) up to which several waves join the parts of one
 struct CachePlan {
   int rows;          // query rows (query x head of the KV group) of a row tile
   int workgroups;
+  int short_tiles;   // where shares would be shorter than this, half as many workgroups share the axis
   int least_tiles;   // a share is not shorter than this
 };
-inline CachePlan choose_cache_plan(int n_requests, int64_t n_rows, int hq, int hkv, int64_t max_q) {
-  (void)n_requests;
-  (void)n_rows;
+// Two workgroups fit a compute unit.  Where each would get but a few tiles, one is given the double: every share costs its start
+// and end and two parts to join (us, 512 / 256 workgroups: one query over 133120 keys, 16 / 2 heads of 128, 8.1 tiles each of
+// 512, 20.3 / 19.3; 256 requests of 65 to 2048 keys, 8 / 2 heads of 64, 9 tiles, 21.6 / 22.9; 64 queries over 16512 keys, 4 tiles,
+// 36 / 34; 64 requests of 512 to 32768 keys, 28 / 4 heads of 128, 56 tiles, 50.6 / 52.0).  Shares of one tile rather than two cost
+// the join more than they save (16000 keys 12.4 / 11.8; 64 queries over 2000 keys 21.6 / 17.4).
+inline CachePlan choose_cache_plan(int hq, int hkv, int d, int64_t max_q) {
   const int64_t rows = max_q * (hq / hkv);
   CachePlan p;
-  p.rows = rows <= 16 ? 16 : 32;
+  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kCacheBlockRows;
   p.workgroups = 512;
-  p.least_tiles = 4;
+  p.short_tiles = d == 128 ? 12 : 6;
+  p.least_tiles = 2;
   return p;
 }
 inline size_t cache_part_bytes(int rows, int d) { return (size_t)rows * (size_t)(d + 2) * sizeof(float); }
@@ -124,8 +137,8 @@ inline size_t cache_attention_workspace_bytes(int n_requests, int64_t n_rows, in
   if (check_heads(1, hq, hkv, d) != APBV_OK || n_requests < 1 || n_requests > APBV_CACHE_MAX_REQUESTS || n_rows < 0 || n_rows > kMaxTokens ||
       n_rows * (hq / hkv) > (int64_t)1 << 30 || max_q < 0 || max_q > kMaxTokens)
     return 0;
-  const CachePlan p = choose_cache_plan(n_requests, n_rows, hq, hkv, max_q);
-  const size_t heads = p.rows == 16 ? 0 : (size_t)kCacheWaves * p.rows * d * sizeof(float);      // pieces that have no room in LDS
+  const CachePlan p = choose_cache_plan(hq, hkv, d, max_q);
+  const size_t heads = p.rows != 32 ? 0 : (size_t)kCacheWaves * p.rows * d * sizeof(float);      // pieces that have no room in LDS
   return align256((size_t)p.workgroups * (2 * cache_part_bytes(p.rows, d) + heads));
 }
 

@@ -32,10 +32,13 @@ int main() {
       for (int n : {1, 7, 64, 4096})
         for (int d : {64, 128}) {
           const int64_t rows = q * n < 1 << 20 ? q * n : 1 << 20;
-          const CachePlan p = choose_cache_plan(n, rows, h[0], h[1], q);
-          CHECK(p.rows >= 16 && p.rows % 16 == 0 && p.workgroups >= 1 && p.least_tiles >= 1);
+          const CachePlan p = choose_cache_plan(h[0], h[1], d, q);
+          CHECK(p.rows >= 16 && p.rows % 16 == 0 && p.workgroups % 16 == 0 && p.least_tiles >= 1);
           CHECK(cache_attention_workspace_bytes(n, rows, h[0], h[1], d, q) >= (size_t)p.workgroups * 2 * p.rows * (d + 2) * 4);
         }
+  // the axis: as many tiles as 32 bits number, and no more
+  CHECK(cache_axis_fits(1, 1, 1, 1, kMaxCachedTokens) && cache_axis_fits(4096, 4096, 28, 4, 1 << 20) && !cache_axis_fits(4096, 4096, 8, 8, kMaxCachedTokens));
+  CHECK(!cache_axis_fits(1, (int64_t)1 << 24, 16, 16, 1 << 20) && cache_axis_fits(64, 8192, 64, 8, 1 << 18));
   CHECK(cache_attention_workspace_bytes(1, (int64_t)1 << 24, 65535, 1, 128, 1) == 0);
   std::printf("cache checks OK\n");
   return 0;

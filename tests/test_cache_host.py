@@ -113,6 +113,7 @@ def test_attention_refuses_bad_arguments_without_launching():
     assert call_attention(q=ApbvTensor(0x1000, 6, 1020, 128, 0)) == -2 and call_attention(q=ApbvTensor(0x1000, 6, 64, 128, 0)) == -2
     assert call_attention(q=ApbvTensor(0x1000, (1 << 24) + 1, 1024, 128, 0)) == -2
     assert call_attention(hq=65534, hkv=1, c=cache(hkv=1), q=ApbvTensor(0x1000, 1 << 17, 65534 * 128, 128, 0)) == -3
+    assert call_attention(n=4096, q=view(4096, 8, 128), blocks=1 << 21, stride=1 << 21) == -3       # more tiles than 32 bits number
     need = apbv.apbv_cache_attention_workspace_bytes(2, 6, 8, 2, 128, 3)
     assert need > 0
     assert call_attention(ws=None) == -4 and call_attention(ws=0x100010) == -4 and call_attention(ws_bytes=need - 1) == -4
