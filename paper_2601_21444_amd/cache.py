@@ -1,4 +1,5 @@
-"""The key/value cache held in 4 bits (include/apbv_cache.h): argument marshalling only, as binding.py for include/apbv.h.
+"""The key/value cache held in 4 bits (include/apbv_cache.h): argument marshalling only, as binding.py for include/apbv.h; the
+plain call is marshalled in native code there and here.
 
 A serving program keeps, for all layers, the block table ``[requests, max_blocks]``, the requests' lengths and the list of free
 pages, and an :class:`ApbvCache` per layer.  A step is ``apbv_cache_map`` once, then in every layer ``apbv_cache_store`` of the
@@ -12,6 +13,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
+from . import binding
 from . import binding
 from .binding import ApbvCacheStruct, ApbvError, _check_buffer, _stream_ptr, load_library, tensor_view
 
@@ -109,6 +111,13 @@ def apbv_cache_map(old_lengths: torch.Tensor, new_lengths: torch.Tensor, block_t
     ``block_table`` and ``free_pages`` are updated in place.  Returns ``(lengths, starts, slots, free_count)``; ``lengths_out``
     may be ``old_lengths`` and ``free_count_out`` ``free_count``, which updates a step's state in place."""
     lib = load_library()
+    if stream is None and lengths_out is not None and starts_out is not None and slots_out is not None and free_count_out is not None:
+        st = binding._native.cache_map(old_lengths, new_lengths, block_table, free_pages, free_count, page_size, max_new_tokens,
+                                       lengths_out, starts_out, slots_out, free_count_out)
+        if st is not None:
+            if st != 0:
+                raise ApbvError(st, "apbv_cache_map")
+            return lengths_out, starts_out, slots_out, free_count_out
     dev = _rows_device(old_lengths, "old_lengths")
     n, max_new = old_lengths.numel(), operator.index(max_new_tokens)
     _check_ints(old_lengths, "old_lengths", (n,), dev)
@@ -140,6 +149,12 @@ def apbv_cache_store(cache: ApbvCache, k: torch.Tensor, v: torch.Tensor, slots: 
     """Writes the rows ``k``, ``v`` ``[tokens, KV heads, d]`` into the cache at ``slots [tokens]``; see apbv_cache_store in
     include/apbv_cache.h.  Returns the cache."""
     lib = load_library()
+    if stream is None and type(cache) is ApbvCache:
+        st = binding._native.cache_store(cache, k, v, slots)
+        if st is not None:
+            if st != 0:
+                raise ApbvError(st, "apbv_cache_store")
+            return cache
     dev = _rows_device(k, "k")
     view, heads, d = _cache_view(cache, dev)
     views = []
@@ -159,6 +174,12 @@ def apbv_cache_load(cache: ApbvCache, slots: torch.Tensor, *, k_out: Optional[to
     """The rows at ``slots [tokens]`` as the bf16 values they stand for, ``(k, v)`` of ``[tokens, KV heads, d]``; see apbv_cache_load in
     include/apbv_cache.h."""
     lib = load_library()
+    if stream is None and type(cache) is ApbvCache and k_out is not None and v_out is not None:
+        st = binding._native.cache_load(cache, slots, k_out, v_out)
+        if st is not None:
+            if st != 0:
+                raise ApbvError(st, "apbv_cache_load")
+            return k_out, v_out
     dev = _rows_device(slots, "slots")
     view, heads, d = _cache_view(cache, dev)
     n = slots.numel()
@@ -188,6 +209,12 @@ def apbv_cache_attention(q: torch.Tensor, cache: ApbvCache, block_table: torch.T
     without ``max_q`` a request is taken to have up to all of them.  Returns ``out [rows, Hq, d]`` bf16 (and ``lse [Hq, rows]``
     fp32), the layouts of apbv_merge_lse."""
     lib = load_library()
+    if stream is None and type(cache) is ApbvCache and out is not None and workspace is not None and not (return_lse and lse_out is None):
+        st = binding._native.cache_attention(q, cache, block_table, lengths, softmax_scale, q_starts, max_q, causal, out, lse_out, workspace)
+        if st is not None:
+            if st != 0:
+                raise ApbvError(st, "apbv_cache_attention")
+            return (out, lse_out) if return_lse else out
     dev = _rows_device(q, "q")
     view, heads, d = _cache_view(cache, dev)
     if q.dim() != 3 or q.shape[2] != d:

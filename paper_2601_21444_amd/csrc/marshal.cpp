@@ -1,7 +1,8 @@
 // Argument marshalling of the Python binding in native code: tensors to apbv_tensor, the checks of the caller's buffers, the
 // current stream, the call.  For the smallest problems the interpreter's time is the call's (one launch takes 2.9 us to
 // enqueue; a call from Python took 3.4 us more for a merge, 7 to 8 us more for an attention).  Enqueueing, before / now
-// (us): merge 6.9 / 3.4, attention 10.5 / 4.8, query attention (two launches) 16.0 / 8.1, compression (three) 15.7 / 8.3.
+// (us): merge 6.9 / 3.4, attention 10.5 / 4.8, query attention (two launches) 16.0 / 8.1, compression (three) 15.7 / 8.3; of the
+// cache's calls attention (two) 15.9 / 5.6, map 9.7 / 3.5, load 10.3 / 3.2.
 //
 // Every function returns the call's status, or None where a call is not the plain case -- an output left to the binding to
 // allocate, an argument of another type, a tensor subclass, any check that fails: the binding then goes the general way,
@@ -10,6 +11,7 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <vector>
 #include "apbv.h"
+#include "apbv_cache.h"
 
 namespace {
 
@@ -272,6 +274,149 @@ PyObject* compress_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- the cache (apbv_cache.h)
+
+// The four tensors of a cache (the binding has looked at its type), pages dense and alike, on a GPU.
+struct Cache {
+  apbv_cache view;
+  int64_t heads, d;
+  c10::Device device = at::kCPU;
+};
+bool cache_of(PyObject* o, Cache& c) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) return false;
+  const at::Tensor* t[4];
+  for (int i = 0; i < 4; ++i) {
+    t[i] = plain(PyTuple_GET_ITEM(o, i));
+    if (t[i] == nullptr || t[i]->scalar_type() != at::kByte || !t[i]->is_cuda() || t[i]->dim() != 4 || t[i]->device() != t[0]->device()) return false;
+  }
+  const auto n = t[0]->sizes();
+  c.heads = n[1];
+  c.d = 2 * n[3];
+  c.device = t[0]->device();
+  for (int i = 0; i < 4; ++i) {
+    const auto m = t[i]->sizes(), s = t[i]->strides();
+    const int64_t width = i < 2 ? n[3] : n[3] / 16;
+    if (m[0] != n[0] || m[1] != n[1] || m[2] != n[2] || m[3] != width || t[i]->numel() == 0) return false;
+    if (s[3] != 1 || s[2] != width || (m[1] > 1 && s[1] != m[2] * width) || s[0] != t[i < 2 ? 0 : 2]->stride(0)) return false;
+  }
+  if (n[2] > 0x7fffffff) return false;
+  c.view = {t[0]->data_ptr(), t[1]->data_ptr(), t[2]->data_ptr(), t[3]->data_ptr(), n[0], t[0]->stride(0), t[2]->stride(0), (int32_t)n[2]};
+  return true;
+}
+// A dense int32 vector of `size` entries on the device (-1: any number, which is returned in it).
+bool ints(PyObject* o, int64_t& size, c10::Device device, int32_t*& ptr) {
+  const at::Tensor* t = plain(o);
+  if (t == nullptr || t->scalar_type() != at::kInt || !t->is_cuda() || t->device() != device || t->dim() != 1 || !t->is_contiguous()) return false;
+  if (size < 0) size = t->numel();
+  ptr = static_cast<int32_t*>(t->data_ptr());
+  return t->numel() == size;
+}
+bool block_table(PyObject* o, int64_t n, c10::Device device, int32_t*& ptr, int64_t& stride, int64_t& blocks) {
+  const at::Tensor* t = plain(o);
+  if (t == nullptr || t->scalar_type() != at::kInt || !t->is_cuda() || t->device() != device || t->dim() != 2 || t->size(0) != n) return false;
+  ptr = static_cast<int32_t*>(t->data_ptr());
+  stride = t->stride(0);
+  blocks = t->size(1);
+  return blocks < 2 || t->stride(1) == 1;
+}
+
+// cache_map(old_lengths, new_lengths, block_table, free_pages, free_count, page_size, max_new_tokens, lengths_out, starts_out, slots_out, free_count_out)
+PyObject* cache_map(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (count != 11) return not_taken();
+  return guarded([&](int& status) {
+    const at::Tensor* first = plain(a[0]);
+    if (first == nullptr || !first->is_cuda()) return false;
+    const c10::Device device = first->device();
+    int64_t n = -1, capacity = -1, one = 1, page, max_new, stride, blocks;
+    int32_t *old_l, *new_l, *free_pages, *free_count, *table;
+    void *lengths, *starts, *slots, *left, *stream;
+    if (!ints(a[0], n, device, old_l) || !ints(a[1], n, device, new_l) || !block_table(a[2], n, device, table, stride, blocks) ||
+        !ints(a[3], capacity, device, free_pages) || !ints(a[4], one, device, free_count) || !whole(a[5], page) || !whole(a[6], max_new) || max_new < 0 || page < 0)
+      return false;
+    for (int i = 7; i < 11; ++i)
+      if (a[i] == Py_None) return false;
+    if (!buffer(a[7], at::kInt, n, device, false, lengths) || !buffer(a[8], at::kInt, n + 1, device, false, starts) ||
+        !buffer(a[9], at::kInt, max_new, device, false, slots) || !buffer(a[10], at::kInt, 1, device, false, left) || !current_stream(stream))
+      return false;
+    Py_BEGIN_ALLOW_THREADS
+    status = apbv_cache_map(to_int(n), to_int(page), blocks, old_l, new_l, table, stride, capacity > 0 ? free_pages : nullptr, capacity, free_count, max_new,
+                            static_cast<int32_t*>(lengths), static_cast<int32_t*>(starts), max_new > 0 ? static_cast<int32_t*>(slots) : nullptr,
+                            static_cast<int32_t*>(left), stream);
+    Py_END_ALLOW_THREADS
+    return true;
+  });
+}
+
+// cache_store(cache, k, v, slots)
+PyObject* cache_store(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (count != 4) return not_taken();
+  return guarded([&](int& status) {
+    Cache c;
+    Tensor k, v;
+    int32_t* slots;
+    void* stream;
+    if (!cache_of(a[0], c) || !view_of(a[1], k, 3) || !view_of(a[2], v, 3) || k.device != c.device || v.device != c.device) return false;
+    if (k.heads != c.heads || v.heads != c.heads || k.d != c.d || v.d != c.d || v.tokens != k.tokens) return false;
+    if (!ints(a[3], k.tokens, c.device, slots) || !current_stream(stream)) return false;
+    Py_BEGIN_ALLOW_THREADS
+    status = apbv_cache_store(&c.view, to_int(c.heads), to_int(c.d), k.view, v.view, k.tokens > 0 ? slots : nullptr, stream);
+    Py_END_ALLOW_THREADS
+    return true;
+  });
+}
+
+// cache_load(cache, slots, k_out, v_out)
+PyObject* cache_load(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (count != 4) return not_taken();
+  return guarded([&](int& status) {
+    Cache c;
+    int64_t n = -1;
+    int32_t* slots;
+    void *k, *v, *stream;
+    if (!cache_of(a[0], c) || !ints(a[1], n, c.device, slots) || a[2] == Py_None || a[3] == Py_None) return false;
+    if (!buffer(a[2], at::kBFloat16, n * c.heads * c.d, c.device, false, k) || !buffer(a[3], at::kBFloat16, n * c.heads * c.d, c.device, false, v) || !current_stream(stream))
+      return false;
+    if (n == 0) slots = nullptr, k = v = nullptr;
+    Py_BEGIN_ALLOW_THREADS
+    status = apbv_cache_load(&c.view, to_int(c.heads), to_int(c.d), n, slots, k, v, stream);
+    Py_END_ALLOW_THREADS
+    return true;
+  });
+}
+
+// cache_attention(q, cache, block_table, lengths, scale, q_starts, max_q, causal, out, lse_out, workspace); q_starts and max_q may be None
+PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (count != 11) return not_taken();
+  return guarded([&](int& status) {
+    Cache c;
+    Tensor q;
+    float scale;
+    int64_t n = -1, max_q = 0, stride, blocks, ws_bytes;
+    int32_t *table, *lengths, *starts = nullptr;
+    void *out, *lse, *ws, *stream;
+    if (!view_of(a[0], q, 3) || !cache_of(a[1], c) || q.device != c.device || q.d != c.d || !ints(a[3], n, c.device, lengths) || n < 1) return false;
+    if (!block_table(a[2], n, c.device, table, stride, blocks) || !number(a[4], scale) || !PyBool_Check(a[7])) return false;
+    if (a[5] != Py_None) {
+      int64_t entries = n + 1;
+      if (!ints(a[5], entries, c.device, starts)) return false;
+    }
+    if (a[6] == Py_None)
+      max_q = starts == nullptr ? q.tokens / n : q.tokens;
+    else if (!whole(a[6], max_q))
+      return false;
+    if (a[8] == Py_None || a[10] == Py_None || !buffer(a[8], at::kBFloat16, q.tokens * q.heads * q.d, c.device, false, out) ||
+        !buffer(a[9], at::kFloat, q.heads * q.tokens, c.device, true, lse) || !buffer(a[10], at::kByte, 0, c.device, false, ws, &ws_bytes) || !current_stream(stream))
+      return false;
+    if (q.tokens == 0) out = nullptr;
+    const int causal = a[7] == Py_True;
+    Py_BEGIN_ALLOW_THREADS
+    status = apbv_cache_attention(&c.view, to_int(n), to_int(q.heads), to_int(c.heads), to_int(c.d), q.view, table, stride, blocks, lengths, starts, max_q, causal, scale,
+                                  out, static_cast<float*>(lse), ws, (size_t)ws_bytes, stream);
+    Py_END_ALLOW_THREADS
+    return true;
+  });
+}
+
 // use_stream(is_initialized, current_device, raw_stream): the functions that name the current stream
 PyObject* use_stream(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 3) {
@@ -288,7 +433,8 @@ PyObject* use_stream(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define APBV_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {APBV_METHOD(merge_lse), APBV_METHOD(host_attention), APBV_METHOD(query_attention), APBV_METHOD(attention_group),
-                         APBV_METHOD(compress_kv), APBV_METHOD(use_stream), {nullptr, nullptr, 0, nullptr}};
+                         APBV_METHOD(compress_kv), APBV_METHOD(cache_map), APBV_METHOD(cache_store), APBV_METHOD(cache_load), APBV_METHOD(cache_attention),
+                         APBV_METHOD(use_stream), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
