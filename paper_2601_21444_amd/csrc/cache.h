@@ -51,7 +51,9 @@ struct CacheAttnParams {
   int64_t table_stride;
   bf16_t* out;             // [n_rows, Hq, d]
   float* lse;              // [Hq, n_rows] or nullptr
-  float* parts;            // [workgroups][2]: O [rows][d] not divided by the row sum, then maxima [rows], row sums [rows]
+  // [workgroups][2][rows][d]: O, not divided by the row sum; then [2][3][rows][workgroups]: maxima, sums of the weights as rounded
+  // for the product with V, and, where the log-sum-exp is wanted, as they were before; then room for pieces (cache_attention.hip)
+  float* parts;
   int n_requests, n_rows, each;     // each: rows of every request where starts is nullptr
   int max_len;             // the longest length a row of the table holds
   int hq, hkv, group, causal;

@@ -132,25 +132,21 @@ apbv_status launch_rows(const CacheRowsParams& p, bool store, hipStream_t stream
 
 constexpr int kMapThreads = 1024;
 constexpr int kMapSlots = 8192;             // new tokens up to which the one workgroup finds the slots too
-constexpr int kMapPerThread = (APBV_CACHE_MAX_REQUESTS + kMapThreads - 1) / kMapThreads;
+constexpr int kTop = 0x7fffffff;
 
 __device__ __forceinline__ int clamp_int(int64_t x, int lo, int hi) { return (int)(x < lo ? lo : (x > hi ? hi : x)); }
 
-// Inclusive sums over the workgroup of three numbers a thread.
-struct Three {
-  int64_t a, b, c;
-};
-__device__ __forceinline__ Three workgroup_scan(Three x, Three* wave_sum) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t a = __shfl_up(x.a, d), b = __shfl_up(x.b, d), c = __shfl_up(x.c, d);
-    if (lane >= d) x.a += a, x.b += b, x.c += c;
-  }
-  if (lane == 63) wave_sum[wave] = x;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) x.a += wave_sum[w].a, x.b += wave_sum[w].b, x.c += wave_sum[w].c;
-  return x;
+// Sums that stop at kTop, over the lanes of a wave (inclusive) on the DPP path.
+__device__ __forceinline__ int add_stop(int x, int y) { return (int)__builtin_elementwise_min(__builtin_elementwise_add_sat((uint32_t)x, (uint32_t)y), (uint32_t)kTop); }
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int dpp_add(int x) { return add_stop(x, __builtin_amdgcn_update_dpp(0, x, kCtrl, kRows, 0xf, false)); }
+__device__ __forceinline__ int wave_scan(int x) {
+  x = dpp_add<0x111, 0xf>(x);      // row_shr 1, 2, 4, 8; row_bcast 15, 31
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);
+  return dpp_add<0x143, 0xc>(x);
 }
 
 // The last b with first[b] <= x among n + 1 ascending entries, first[0] = 0 <= x < first[n].
@@ -165,110 +161,167 @@ __device__ __forceinline__ int owner(const int* first, int n, int x) {
 
 // The slot of position pos, whose block lies on this page; -1 where no slot has that number.
 __device__ __forceinline__ int slot_of(int page, int pos, int page_log2) {
-  if (page < 0 || page > (0x7fffffff >> page_log2)) return -1;
+  if (page < 0 || page > (kTop >> page_log2)) return -1;
   return (page << page_log2) + (pos & ((1 << page_log2) - 1));
 }
 
-// What a request asks for.
-struct Change {
-  int had, want;           // lengths; the same where the new length cannot be taken at all
-  int64_t grown;           // new tokens
-  __device__ __forceinline__ Change(const CacheMapParams& p, int b) {
-    had = clamp_int(p.old_lengths[b], 0, p.cap);
-    const int n = p.new_lengths[b];
-    grown = (int64_t)n > had ? (int64_t)n - had : 0;
-    want = n < 0 || n > p.cap ? had : n;
-  }
-  __device__ __forceinline__ int blocks(const CacheMapParams& p, int length) const { return (int)(((int64_t)length + (1 << p.page_log2) - 1) >> p.page_log2); }
-};
-
+// One workgroup.  A thread holds kPer consecutive requests in registers and knows, after the prefix sums, where their tokens and
+// pages lie.  In a decoding step, where no request grows by more than kFew tokens, that is all it takes: every thread serves
+// its own requests.  Otherwise, and for pages given back, tokens and pages are dealt to the threads, which find the request of
+// each in LDS.  Pages are taken from where the list has them or will have them, so that nothing written here is read here: two
+// waits for memory in all, for the lengths and for the pages.
+template <int kPer>
 __global__ __launch_bounds__(kMapThreads) void cache_map_kernel(const CacheMapParams p, const int with_slots) {
-  // first new token, first page taken and first page given back of every request, cut off at 2^31 - 1
-  __shared__ int first_token[APBV_CACHE_MAX_REQUESTS + 1], first_taken[APBV_CACHE_MAX_REQUESTS + 1], first_back[APBV_CACHE_MAX_REQUESTS + 1];
-  __shared__ Three wave_sum[kMapThreads / 64];
+  constexpr int kMost = kPer * kMapThreads, kWaves = kMapThreads / 64;
+  constexpr int kFew = 4;                      // fewer than a page: at most one page is taken
+  // first new token, first page taken and first page given back of every request (sums that stop at kTop), and its old length,
+  // with the upper bit set where it is granted
+  __shared__ int first_token[kMost + 1], first_taken[kMost + 1], first_back[kMost + 1];
+  __shared__ uint32_t had_granted[kMost];
+  __shared__ int wave_sum[kWaves][4];          // the three sums, and whether a request grows by many tokens
   __shared__ int n_taken;
-  const int n = p.n_requests, per = (n + kMapThreads - 1) / kMapThreads;
-  if (threadIdx.x == 0) n_taken = 0;
+  const int n = p.n_requests, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b0 = threadIdx.x * kPer;
+  auto blocks = [&](int length) { return (int)(((uint32_t)length + (1u << p.page_log2) - 1) >> p.page_log2); };
+  auto table_at = [&](int b, int block) -> int32_t* { return p.table + (int64_t)b * p.table_stride + block; };
 
-  Three mine = {0, 0, 0};
-  for (int u = 0; u < per; ++u) {
-    const int b = threadIdx.x * per + u;
-    if (b >= n) break;
-    const Change c(p, b);
-    const int up = c.blocks(p, c.want) - c.blocks(p, c.had);
-    mine.a += c.grown;
-    mine.b += up > 0 ? up : 0;
-    mine.c += up < 0 ? -up : 0;
+  const int held = clamp_int(*p.free_count, 0, p.free_capacity);
+  int had[kPer], want[kPer], grown[kPer];      // want: as asked for; the old length where that cannot be taken at all
+  bool possible[kPer];
+  int sum[3] = {0, 0, 0};
+  bool many = false;
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    const int b = b0 + u < n ? b0 + u : n - 1;
+    had[u] = p.old_lengths[b];
+    want[u] = p.new_lengths[b];
   }
-  Three at = workgroup_scan(mine, wave_sum);
-  at.a -= mine.a, at.b -= mine.b, at.c -= mine.c;
-  constexpr int kTop = 0x7fffffff;
-  for (int u = 0; u <= per; ++u) {
-    const int b = threadIdx.x * per + u;
-    if (b > n || (u == per && b != n)) break;              // (the last thread's entry behind its own: the totals)
-    first_token[b] = clamp_int(at.a, 0, kTop);
-    first_taken[b] = clamp_int(at.b, 0, kTop);
-    first_back[b] = clamp_int(at.c, 0, kTop);
-    if (b == n) break;
-    const Change c(p, b);
-    const int up = c.blocks(p, c.want) - c.blocks(p, c.had);
-    at.a += c.grown;
-    at.b += up > 0 ? up : 0;
-    at.c += up < 0 ? -up : 0;
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    const bool real = b0 + u < n;
+    had[u] = clamp_int(had[u], 0, p.cap);
+    grown[u] = real && want[u] > had[u] ? want[u] - had[u] : 0;
+    many = many || grown[u] > kFew;
+    possible[u] = want[u] >= 0 && want[u] <= p.cap;
+    if (!possible[u] || !real) want[u] = had[u];
+    const int up = blocks(want[u]) - blocks(had[u]);
+    sum[0] = add_stop(sum[0], grown[u]);
+    sum[1] = add_stop(sum[1], up > 0 ? up : 0);
+    sum[2] = add_stop(sum[2], up < 0 ? -up : 0);
+  }
+  int at[3];                                   // behind this thread's requests, then before each of them
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    at[k] = wave_scan(sum[k]);
+    if (lane == 63) wave_sum[wave][k] = at[k];
+  }
+  const bool wave_many = __builtin_amdgcn_ballot_w64(many) != 0;
+  if (lane == 63) wave_sum[wave][3] = wave_many;
+  if (threadIdx.x == 0) n_taken = 0;
+  __syncthreads();
+  // (exclusive over the wave's lanes: the inclusive sum of the lane before, as sums that stop cannot be taken back)
+  int total[4] = {0, 0, 0, 0}, before[3];
+  const int waves = (n + 64 * kPer - 1) / (64 * kPer);     // those that hold requests
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    before[k] = __shfl_up(at[k], 1);
+    before[k] = lane == 0 ? 0 : before[k];
+  }
+  for (int w = 0; w < waves; ++w) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int x = wave_sum[w][k];
+      if (k < 3 && w < wave) before[k < 3 ? k : 0] = add_stop(before[k < 3 ? k : 0], x);
+      total[k] = add_stop(total[k], x);
+    }
+  }
+  const int n_back = total[2];
+  const bool own = total[3] == 0;              // every thread serves its own requests
+  const int free = clamp_int((int64_t)held + n_back, 0, p.free_capacity);
+
+  // Refused for want of pages or room: what is asked for up to a request only grows, so that the pages taken are a prefix of
+  // those asked for.
+  int first[3][kPer];
+  bool granted[kPer];
+  int last_taken = 0;
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    const int b = b0 + u, up = blocks(want[u]) - blocks(had[u]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) first[k][u] = before[k];
+    before[0] = add_stop(before[0], grown[u]);
+    before[1] = add_stop(before[1], up > 0 ? up : 0);
+    before[2] = add_stop(before[2], up < 0 ? -up : 0);
+    granted[u] = possible[u] && (grown[u] == 0 || (before[0] <= p.max_new && (up == 0 || before[1] <= free)));
+    if (granted[u] && up > 0) last_taken = before[1];
+    if (b < n) {
+      p.lengths_out[b] = granted[u] ? want[u] : had[u];
+      p.starts_out[b] = first[0][u] < p.max_new ? first[0][u] : p.max_new;
+    }
+  }
+  if (threadIdx.x == 0) p.starts_out[n] = total[0] < p.max_new ? total[0] : p.max_new;
+  if (last_taken > 0) atomicMax(&n_taken, last_taken);
+  if (!own || n_back > 0) {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int b = b0 + u;
+      if (b > n) continue;
+      first_token[b] = first[0][u];
+      first_taken[b] = first[1][u];
+      first_back[b] = first[2][u];
+      if (b < n) had_granted[b] = (uint32_t)had[u] | (granted[u] ? 0x80000000u : 0u);
+    }
+    if (threadIdx.x == 0) first_token[n] = total[0], first_taken[n] = total[1], first_back[n] = total[2];
   }
   __syncthreads();
-  const int held = clamp_int(*p.free_count, 0, p.free_capacity);
-  const int n_back = first_back[n];
+  if (threadIdx.x == 0) *p.free_count_out = free - n_taken;
 
-  // pages given back, behind the free ones
-  for (int i = threadIdx.x; i < n_back && i < p.free_capacity - held; i += kMapThreads) {
+  // a page given back, the i-th: one of the last blocks its request had; entry i of the list as it stands then
+  auto back = [&](int i) -> const int32_t* {
     const int b = owner(first_back, n, i);
-    const Change c(p, b);
-    p.free_pages[held + i] = p.table[(int64_t)b * p.table_stride + c.blocks(p, c.want) + (i - first_back[b])];
-  }
-  const int free = clamp_int((int64_t)held + n_back, 0, p.free_capacity);
-  // Refused for want of pages or room: what is asked for up to a request only grows, so that the pages taken are a prefix
-  // of those asked for.
-  auto granted = [&](int b, const Change& c) {
-    if (p.new_lengths[b] != c.want) return false;
-    if (c.grown == 0) return true;
-    return first_token[b + 1] <= p.max_new && (first_taken[b + 1] == first_taken[b] || first_taken[b + 1] <= free);
+    return table_at(b, blocks((int)(had_granted[b] & kTop)) - (first_back[b + 1] - i));
   };
-  for (int b = threadIdx.x; b < n; b += kMapThreads) {
-    const Change c(p, b);
-    if (granted(b, c) && c.grown > 0) atomicMax(&n_taken, first_taken[b + 1] <= free ? first_taken[b + 1] : 0);
-  }
-  __syncthreads();                                         // ... and the free pages written above can be read
-  const int taken = n_taken;
-  for (int i = threadIdx.x; i < taken; i += kMapThreads) {
-    const int b = owner(first_taken, n, i);
-    const Change c(p, b);
-    p.table[(int64_t)b * p.table_stride + c.blocks(p, c.had) + (i - first_taken[b])] = p.free_pages[free - 1 - i];
-  }
-  for (int b = threadIdx.x; b <= n; b += kMapThreads) p.starts_out[b] = first_token[b] < p.max_new ? first_token[b] : p.max_new;
-  __syncthreads();                                         // the table is complete
-  if (with_slots) {
-    const int total = first_token[n];
-    for (int t = threadIdx.x; t < p.max_new; t += kMapThreads) {
-      int slot = -1;
-      if (t < total) {
-        const int b = owner(first_token, n, t);
-        const Change c(p, b);
-        if (granted(b, c)) {
-          const int pos = c.had + (t - first_token[b]);
-          slot = slot_of(p.table[(int64_t)b * p.table_stride + (pos >> p.page_log2)], pos, p.page_log2);
-        }
+  auto entry = [&](int i) -> const int32_t* { return i < held ? p.free_pages + i : back(i - held); };
+
+  if (own) {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int b = b0 + u, old = blocks(had[u]), up = blocks(want[u]) - old;
+      if (b >= n || grown[u] == 0) continue;
+      int page_old = -1, page_new = -1;
+      if (granted[u]) {
+        if ((had[u] & ((1 << p.page_log2) - 1)) != 0) page_old = *table_at(b, old - 1);
+        if (up > 0) page_new = *entry(free - 1 - first[1][u]);
+        if (up > 0) *table_at(b, old) = page_new;
       }
-      p.slots_out[t] = slot;
+      if (with_slots)
+        for (int j = 0; j < grown[u]; ++j) {
+          const int pos = had[u] + j;
+          if (first[0][u] + j < p.max_new)
+            p.slots_out[first[0][u] + j] = granted[u] ? slot_of(pos >> p.page_log2 < old ? page_old : page_new, pos, p.page_log2) : -1;
+        }
     }
-    __syncthreads();                                       // (lengths_out may be old_lengths)
+    if (with_slots)
+      for (int t = total[0] + threadIdx.x; t >= 0 && t < p.max_new; t += kMapThreads) p.slots_out[t] = -1;
+  } else {
+    const int taken = n_taken;
+    for (int i = threadIdx.x; i < taken; i += kMapThreads) {
+      const int b = owner(first_taken, n, i);
+      *table_at(b, blocks((int)(had_granted[b] & kTop)) + (i - first_taken[b])) = *entry(free - 1 - i);
+    }
+    if (with_slots)
+      for (int t = threadIdx.x; t < p.max_new; t += kMapThreads) {
+        int slot = -1;
+        if (t < total[0]) {
+          const int b = owner(first_token, n, t);
+          if (had_granted[b] >> 31) {
+            const int old = (int)(had_granted[b] & kTop), pos = old + (t - first_token[b]), block = pos >> p.page_log2, fresh = block - blocks(old);
+            slot = slot_of(fresh >= 0 ? *entry(free - 1 - first_taken[b] - fresh) : *table_at(b, block), pos, p.page_log2);
+          }
+        }
+        p.slots_out[t] = slot;
+      }
   }
-  if (threadIdx.x == 0) *p.free_count_out = free - taken;
-  // (a request's lengths are read by the thread that writes its result, and by no other any more)
-  for (int b = threadIdx.x; b < n; b += kMapThreads) {
-    const Change c(p, b);
-    p.lengths_out[b] = granted(b, c) ? c.want : c.had;
-  }
+  for (int i = threadIdx.x; i < n_back && i < p.free_capacity - held; i += kMapThreads) p.free_pages[held + i] = *back(i);
 }
 
 // The slots of many new tokens, from what the first launch wrote: a request that was refused kept another length than it
@@ -309,7 +362,8 @@ apbv_status launch_cache_load(const CacheRowsParams& p, int head_dim, hipStream_
 apbv_status launch_cache_map(const CacheMapParams& p, hipStream_t stream) {
   Launcher launch(stream);
   const int with_slots = p.max_new <= kMapSlots;
-  launch(cache_map_kernel, dim3(1), dim3(kMapThreads), 0, p, with_slots);
+  static_assert(4 * kMapThreads == APBV_CACHE_MAX_REQUESTS, "a thread's requests");
+  launch(p.n_requests <= kMapThreads ? cache_map_kernel<1> : cache_map_kernel<4>, dim3(1), dim3(kMapThreads), 0, p, with_slots);
   if (!with_slots) {
     const unsigned per = 256 * kSlotsPerThread;
     launch(cache_slots_kernel, dim3(((unsigned)p.max_new + per - 1) / per), dim3(256), 0, p);

@@ -22,7 +22,9 @@ namespace {
 
 enum : int { kHead = 1, kTail = 2, kSpan = 4 };            // what a wave keeps of row tiles that are not its own alone
 
-template <int D, int NQ, bool kOnePage>
+// kLse: the log-sum-exp is wanted, and the weights are added up before they are rounded, too: their rounded sum, which the
+// output is divided by, would leave it with errors of 2^-9 over the square root of the number of keys.
+template <int D, int NQ, bool kOnePage, bool kLse>
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(const CacheAttnParams p) {
   using T = Tile<D, 1>;
   constexpr int W = kCacheWaves, R = 16 * NQ;
@@ -31,7 +33,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
   constexpr int kWaveLds = T::TILE_BYTES > R * D * 4 ? T::TILE_BYTES : R * D * 4;
   constexpr bool kHeadsInLds = NQ == 1;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kHeadsInLds ? 2 : 1][W][kWaveLds];      // [tails, heads]
-  __shared__ float stat[2][W][2][R];                       // [tails, heads][wave][maximum, row sum]
+  __shared__ float stat[2][W][3][R];                       // [tails, heads][wave][maximum, row sum, exact row sum]
   __shared__ __attribute__((aligned(16))) int kept[W], place[2][W][4];       // place: first query, rows, KV head, first row
 
   const int lane = threadIdx.x & 63;
@@ -60,7 +62,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     for (int d = 0; d < T::DBN; ++d) v_off[d] = row * T::ROW_BYTES + (((2 * d + ((li & 3) >> 1)) ^ T::fv(row)) << 4) + (li & 1) * 8;
   }
   constexpr int kChunks = D / 4;                           // 16-byte chunks of a kept row of O, swizzled by the row
-  float* head_global = p.parts + (int64_t)p.workgroups * 2 * (R * (D + 2)) + (int64_t)wg * W * (R * D);
+  float* head_global = p.parts + (int64_t)p.workgroups * 2 * (R * (D + 3)) + (int64_t)wg * W * (R * D);
   unsigned char* vbuf = lds[0][wave];
   const float inv_scale_log2 = 1.0f / p.scale_log2;
 
@@ -107,13 +109,13 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     const int t_end = some <= 0 ? 0 : (t1 * kCacheKeyTile < some ? t1 : (some + kCacheKeyTile - 1) / kCacheKeyTile);
 
     f32x4 o[T::DBN][NQ];
-    float m_ref[NQ], m_sub[NQ], s_far[NQ], l_run[NQ];
+    float m_ref[NQ], m_sub[NQ], s_far[NQ], l_run[NQ], e_run[NQ];
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
 #pragma unroll
       for (int d = 0; d < T::DBN; ++d) o[d][nq] = f32x4{0.f, 0.f, 0.f, 0.f};
       m_ref[nq] = s_far[nq] = -INFINITY;
-      m_sub[nq] = l_run[nq] = 0.f;
+      m_sub[nq] = l_run[nq] = e_run[nq] = 0.f;
     }
 
     const int32_t* table_row = p.table + (int64_t)b * p.table_stride;
@@ -189,6 +191,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
           m_sub[nq] = m_new > -INFINITY ? m_new : 0.f;
           s_far[nq] = (m_new + kRescaleThreshold) * inv_scale_log2;
           l_run[nq] *= alpha;
+          if constexpr (kLse) e_run[nq] *= alpha;
 #pragma unroll
           for (int d = 0; d < T::DBN; ++d) o[d][nq] *= alpha;
         }
@@ -212,6 +215,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
               const f32x4& y = s[2 * half + mb][nq];
               const f32x2 xy = {__builtin_amdgcn_exp2f(__builtin_fmaf(y[e], p.scale_log2, -m_sub[nq])),
                                 __builtin_amdgcn_exp2f(__builtin_fmaf(y[e + 1], p.scale_log2, -m_sub[nq]))};
+              if constexpr (kLse) e_run[nq] += xy.x + xy.y;
               const bf16x2 c = __builtin_convertvector(xy, bf16x2);
               l_run[nq] = __builtin_amdgcn_fdot2_f32_bf16(c, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l_run[nq], false);
               pw[nq][2 * mb + (e >> 1)] = __builtin_bit_cast(uint32_t, c);
@@ -248,10 +252,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     }
 
     // ---- a piece that is a whole row tile is done; others are kept for the waves' pieces to be put together below
-    float l_tot[NQ];
-#pragma unroll
-    for (int nq = 0; nq < NQ; ++nq) {
-      float x = l_run[nq];
+    auto over_quarters = [](float x) {
       {
         auto sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
         x = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
@@ -260,7 +261,13 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
         auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
         x = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
       }
-      l_tot[nq] = x;
+      return x;
+    };
+    float l_tot[NQ], e_tot[NQ];
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+      l_tot[nq] = over_quarters(l_run[nq]);
+      e_tot[nq] = kLse ? over_quarters(e_run[nq]) : 0.f;
     }
     if (t0 == 0 && t1 == rq.tiles) {
 #pragma unroll
@@ -278,8 +285,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
           y.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x.z, x.w}), bf16x2));
           *reinterpret_cast<u32x2*>(dst + 16 * d) = y;
         }
-        if (p.lse != nullptr && lg == 0)
-          p.lse[(int64_t)h * p.n_rows + rq.first + i] = l_tot[nq] > 0.f ? (m_ref[nq] + __builtin_amdgcn_logf(l_tot[nq])) * 0.6931471805599453f : -INFINITY;
+        if (kLse && lg == 0) p.lse[(int64_t)h * p.n_rows + rq.first + i] = log_sum(m_ref[nq], e_tot[nq]);
       }
     } else {
       // (a row tile that ends here but began before is a head; one that goes on, a tail or, of one that began before, a span)
@@ -301,6 +307,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
         for (int nq = 0; nq < NQ; ++nq) {
           stat[is_head][wave][0][16 * nq + li] = m_ref[nq];
           stat[is_head][wave][1][16 * nq + li] = l_tot[nq];
+          if (kLse) stat[is_head][wave][2][16 * nq + li] = e_tot[nq];
         }
       }
       keeps |= is_head ? kHead : (t0 == 0 ? kTail : kSpan);
@@ -341,11 +348,11 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     const int first = at[0], rows = at[1], head = at[2], r0 = at[3];
     const int slot = chain > 0 ? 1 : 0;                    // a part that begins a row tile, or one that goes on with it
     float* part = p.parts + ((int64_t)wg * 2 + slot) * (R * D);
-    float* part_stat = p.parts + (int64_t)p.workgroups * 2 * (R * D) + (int64_t)slot * (2 * R) * p.workgroups + wg;
+    float* part_stat = part_stats(p, slot, R, D) + wg;
     for (int x = threadIdx.x; x < R * (D / 8); x += 64 * W) {
       const int row = x / (D / 8), c = x % (D / 8);
       if (r0 + row >= rows) break;
-      float m = -INFINITY, l = 0.f;
+      float m = -INFINITY, l = 0.f, exact = 0.f;
       for (int w = from; w <= to; ++w) m = fmaxf(m, stat[w == to && ends ? 1 : 0][w][0][row]);
       const float m0 = m > -INFINITY ? m : 0.f;
       f32x4 x0 = {0.f, 0.f, 0.f, 0.f}, x1 = {0.f, 0.f, 0.f, 0.f};
@@ -353,6 +360,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
         const int is_head = w == to && ends ? 1 : 0;
         const float weight = __builtin_amdgcn_exp2f(stat[is_head][w][0][row] - m0);
         l = __builtin_fmaf(stat[is_head][w][1][row], weight, l);
+        if (kLse) exact = __builtin_fmaf(stat[is_head][w][2][row], weight, exact);
         auto add = [&](const f32x4* src) {
           src += row * kChunks;
           x0 += weight * src[(2 * c) ^ (row & 15)];
@@ -376,8 +384,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
         y.w = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x1.z, x1.w}), bf16x2));
         const int i = (r0 + row) / p.group, h = head * p.group + (r0 + row) % p.group;
         *reinterpret_cast<u32x4*>(p.out + ((int64_t)(first + i) * p.hq + h) * D + 8 * c) = y;
-        if (p.lse != nullptr && c == 0)
-          p.lse[(int64_t)h * p.n_rows + first + i] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+        if (kLse && c == 0) p.lse[(int64_t)h * p.n_rows + first + i] = log_sum(m, exact);
       } else {
         f32x4* dst = reinterpret_cast<f32x4*>(part + row * D + 8 * c);
         dst[0] = x0;
@@ -385,6 +392,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
         if (c == 0) {
           part_stat[(int64_t)row * p.workgroups] = m;
           part_stat[(int64_t)(R + row) * p.workgroups] = l;
+          if (kLse) part_stat[(int64_t)(2 * R + row) * p.workgroups] = exact;
         }
       }
     }
@@ -397,7 +405,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
 template <int D, int R, int kJoin>
 __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kernel(const CacheAttnParams p) {
   constexpr int kRowsPerGroup = kJoin == 1 ? 4 : 1;
-  __shared__ float shared_max[kJoin], shared_sum[kJoin];
+  __shared__ float shared_max[kJoin], shared_sum[kJoin], shared_exact[kJoin];
   __shared__ f32x4 shared_acc[kJoin][D / 4];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -413,7 +421,8 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
   constexpr int kAtOnce = 64 / kLanes;
   const int sub = lane / kLanes, c = lane % kLanes;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, exact = 0.f;               // exact: of the weights before they were rounded, for the log-sum-exp
+  const bool with_lse = p.lse != nullptr;
   if (rq.tiles > 0) {
     const uint32_t share = axis.share(p);
     const int r = i * p.group + h % p.group, rt = r / R, row_tiles = (rq.rows + R - 1) / R;
@@ -422,7 +431,7 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
     int last = (int)((from + rq.tiles - 1) / share);
     last = last < p.workgroups ? last : p.workgroups - 1;
     if (first == last) return;                             // written by its only workgroup
-    const float* stat = p.parts + (int64_t)p.workgroups * 2 * (R * D) + (int64_t)(r % R) * p.workgroups;
+    const float* stat = part_stats(p, 0, R, D) + (int64_t)(r % R) * p.workgroups;
     const float* rows = p.parts + (r % R) * D + 4 * c;
     // a wave's equal share of the parts, kAtOnce * kLoads at a time: lane n holds the n-th's maximum and row sum, and the rows
     // are on their way while the weights are found
@@ -433,8 +442,9 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
     for (int base = from_part; base < past_part; base += kChunk) {
       const int w = base + lane;
       const bool mine = lane < kChunk && w < past_part;
-      const float* s = stat + (w == first ? (int64_t)(2 * R) * p.workgroups : 0) + w;
+      const float* s = stat + (w == first ? (int64_t)(3 * R) * p.workgroups : 0) + w;
       const float m_part = mine ? s[0] : -INFINITY, l_part = mine ? s[(int64_t)R * p.workgroups] : 0.f;
+      const float exact_part = mine && with_lse ? s[(int64_t)(2 * R) * p.workgroups] : 0.f;
       f32x4 x[kLoads];
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {
@@ -450,19 +460,23 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
       const float old = __builtin_amdgcn_exp2f(m - m0), weight = __builtin_amdgcn_exp2f(m_part - m0);
       m = top;
       l = __builtin_fmaf(l, old, weight * l_part);         // (this lane's parts; the lanes are added up below)
+      exact = __builtin_fmaf(exact, old, weight * exact_part);
       acc *= old;
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) acc += __shfl(weight, u * kAtOnce + sub) * x[u];
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
+    if (with_lse)
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) exact += __shfl_xor(exact, d);
 #pragma unroll
     for (int d = kLanes; d < 64; d *= 2)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], d);
   }
   if constexpr (kJoin > 1) {
-    if (lane == 0) shared_max[wave] = m, shared_sum[wave] = l;
+    if (lane == 0) shared_max[wave] = m, shared_sum[wave] = l, shared_exact[wave] = exact;
     if (sub == 0) shared_acc[wave][c] = acc;
     __syncthreads();
     if (wave != 0) return;
@@ -470,12 +484,13 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
 #pragma unroll
     for (int w = 0; w < kJoin; ++w) m = fmaxf(m, shared_max[w]);
     const float m0 = m > -INFINITY ? m : 0.f;
-    l = 0.f;
+    l = exact = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kJoin; ++w) {
       const float weight = __builtin_amdgcn_exp2f(shared_max[w] - m0);
       l = __builtin_fmaf(shared_sum[w], weight, l);
+      exact = __builtin_fmaf(shared_exact[w], weight, exact);
       acc += weight * shared_acc[w][c];
     }
   }
@@ -485,7 +500,7 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
   y.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc.x * inv, acc.y * inv}), bf16x2));
   y.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc.z * inv, acc.w * inv}), bf16x2));
   *reinterpret_cast<u32x2*>(p.out + job * D + 4 * c) = y;
-  if (p.lse != nullptr && lane == 0) p.lse[(int64_t)h * p.n_rows + row] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+  if (with_lse && lane == 0) p.lse[(int64_t)h * p.n_rows + row] = log_sum(m, exact);
 }
 
 template <int D, int R>
@@ -496,21 +511,26 @@ void launch_join(Launcher& launch, const CacheAttnParams& p) {
   else
     launch(cache_join_kernel<D, R, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, p);
 }
+template <int D, int NQ>
+void launch_few_rows(Launcher& launch, const CacheAttnParams& p) {
+  const bool one_page = (1 << p.cache.page_log2) >= kCacheKeyTile;
+  auto kernel = one_page ? (p.lse ? cache_attention_kernel<D, NQ, true, true> : cache_attention_kernel<D, NQ, true, false>)
+                         : (p.lse ? cache_attention_kernel<D, NQ, false, true> : cache_attention_kernel<D, NQ, false, false>);
+  launch(kernel, dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
+  launch_join<D, 16 * NQ>(launch, p);
+}
 template <int D>
 apbv_status launch_dim(const CacheAttnParams& p, int rows, hipStream_t stream) {
   if ((int64_t)p.n_rows * p.hq > 0x7fffffff) return APBV_ERR_UNSUPPORTED;
   Launcher launch(stream);
-  const bool one_page = (1 << p.cache.page_log2) >= kCacheKeyTile;
-  if (rows == kCacheBlockRows) {
+  if (rows == 16) {
+    launch_few_rows<D, 1>(launch, p);
+  } else if (rows == 32) {
+    launch_few_rows<D, 2>(launch, p);
+  } else {
     const apbv_status st = launch_cache_block_attention(p, D, stream);
     if (st != APBV_OK) return st;
     launch_join<D, kCacheBlockRows>(launch, p);
-  } else if (rows == 32) {
-    launch(one_page ? cache_attention_kernel<D, 2, true> : cache_attention_kernel<D, 2, false>, dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
-    launch_join<D, 32>(launch, p);
-  } else {
-    launch(one_page ? cache_attention_kernel<D, 1, true> : cache_attention_kernel<D, 1, false>, dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
-    launch_join<D, 16>(launch, p);
   }
   return launch.status();
 }

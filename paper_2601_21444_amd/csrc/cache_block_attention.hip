@@ -28,7 +28,7 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <int D>
+template <int D, bool kLse>                                // kLse: as in cache_attention.hip
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_kernel(const CacheAttnParams p) {
   using T = Tile<D, 1, true>;
   constexpr int W = kCacheWaves, R = kCacheBlockRows;
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_ker
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
-    float m_ref = -INFINITY, m_sub = 0.f, s_far = -INFINITY, l_run = 0.f;
+    float m_ref = -INFINITY, m_sub = 0.f, s_far = -INFINITY, l_run = 0.f, e_run = 0.f;
     const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
     bf16x8 kf[KS];
@@ -189,6 +189,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_ker
         m_sub = m_new > -INFINITY ? m_new : 0.f;
         s_far = (m_new + kRescaleThreshold) * inv_scale_log2;
         l_run *= alpha;
+        if constexpr (kLse) e_run *= alpha;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -219,6 +220,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_ker
       };
       auto stage_c = [&](int pi) {
         const f32x2 xy = {xf[pi][0], xf[pi][1]};
+        if constexpr (kLse) e_run += xy.x + xy.y;
         cw[pi] = __builtin_bit_cast(uint32_t, __builtin_convertvector(xy, bf16x2));
         pw[pi >> 2][pi & 3] = cw[pi];
       };
@@ -368,10 +370,14 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_ker
     const bool whole = t0 == 0 && t1 == rq.tiles;
     const int part_slot = t0 == 0 ? 1 : 0;
     float* part = p.parts + ((int64_t)wg * 2 + part_slot) * (R * D);
-    float* part_stat = p.parts + (int64_t)p.workgroups * 2 * (R * D) + (int64_t)part_slot * (2 * R) * p.workgroups + wg;
+    float* part_stat = part_stats(p, part_slot, R, D) + wg;
     {
       auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
       l_run = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    }
+    if constexpr (kLse) {
+      auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(e_run), __float_as_uint(e_run), false, false);
+      e_run = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
     }
     if (rw + c >= rq.rows) continue;
     if (whole) {
@@ -387,8 +393,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_ker
           y.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[db][4 * q + 2] * inv, o[db][4 * q + 3] * inv}), bf16x2));
           *reinterpret_cast<u32x2*>(dst + 32 * db + 8 * q) = y;
         }
-      if (p.lse != nullptr && hh == 0)
-        p.lse[(int64_t)h * p.n_rows + rq.first + qi] = l_run > 0.f ? (m_ref + __builtin_amdgcn_logf(l_run)) * 0.6931471805599453f : -INFINITY;
+      if (kLse && hh == 0) p.lse[(int64_t)h * p.n_rows + rq.first + qi] = log_sum(m_ref, e_run);
     } else {
       const int in_tile = 32 * wave + c;
 #pragma unroll
@@ -399,6 +404,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_ker
       if (hh == 0) {
         part_stat[(int64_t)in_tile * p.workgroups] = m_ref;
         part_stat[(int64_t)(R + in_tile) * p.workgroups] = l_run;
+        if (kLse) part_stat[(int64_t)(2 * R + in_tile) * p.workgroups] = e_run;
       }
     }
   }
@@ -408,7 +414,9 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_ker
 
 apbv_status launch_cache_block_attention(const CacheAttnParams& p, int head_dim, hipStream_t stream) {
   Launcher launch(stream);
-  launch(head_dim == 128 ? cache_block_attention_kernel<128> : cache_block_attention_kernel<64>, dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
+  auto kernel = head_dim == 128 ? (p.lse ? cache_block_attention_kernel<128, true> : cache_block_attention_kernel<128, false>)
+                                : (p.lse ? cache_block_attention_kernel<64, true> : cache_block_attention_kernel<64, false>);
+  launch(kernel, dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
   return launch.status();
 }
 

@@ -41,6 +41,17 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
   return x;
 }
 
+// Natural logarithm of l * 2^m: the result is held to what float32 holds, whatever the sizes of m and l.
+__device__ __forceinline__ float log_sum(float m, float l) {
+  if (!(l > 0.f)) return -INFINITY;
+  const double x = (double)m + (double)__builtin_amdgcn_frexp_expf(l) + (double)__builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(l));
+  return (float)(x * 0.69314718055994530942);
+}
+// Statistics of the parts of a workgroup that begin a row tile (slot 1) or go on with one (slot 0): maxima, sums, exact sums.
+__device__ __forceinline__ float* part_stats(const CacheAttnParams& p, int slot, int R, int D) {
+  return p.parts + (int64_t)p.workgroups * 2 * (R * D) + (int64_t)slot * (3 * R) * p.workgroups;
+}
+
 // The axis of tiles: its length, and where the requests lie on it.  A wave holds a window of 64 consecutive requests, one a
 // lane, handed from lane to lane as they are needed; with more than 64 it first adds up 64 groups of `per` (at most 64).
 // The host has seen that the tiles of requests which do not overlap fit 32 bits; sums stop at the largest number otherwise.

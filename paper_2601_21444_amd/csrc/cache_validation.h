@@ -132,7 +132,7 @@ inline CachePlan choose_cache_plan(int hq, int hkv, int d, int64_t max_q) {
   p.least_tiles = 2;
   return p;
 }
-inline size_t cache_part_bytes(int rows, int d) { return (size_t)rows * (size_t)(d + 2) * sizeof(float); }
+inline size_t cache_part_bytes(int rows, int d) { return (size_t)rows * (size_t)(d + 3) * sizeof(float); }
 inline size_t cache_attention_workspace_bytes(int n_requests, int64_t n_rows, int hq, int hkv, int d, int64_t max_q) {
   if (check_heads(1, hq, hkv, d) != APBV_OK || n_requests < 1 || n_requests > APBV_CACHE_MAX_REQUESTS || n_rows < 0 || n_rows > kMaxTokens ||
       n_rows * (hq / hkv) > (int64_t)1 << 30 || max_q < 0 || max_q > kMaxTokens)

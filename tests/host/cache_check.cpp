@@ -34,7 +34,7 @@ int main() {
           const int64_t rows = q * n < 1 << 20 ? q * n : 1 << 20;
           const CachePlan p = choose_cache_plan(h[0], h[1], d, q);
           CHECK(p.rows >= 16 && p.rows % 16 == 0 && p.workgroups % 16 == 0 && p.least_tiles >= 1);
-          CHECK(cache_attention_workspace_bytes(n, rows, h[0], h[1], d, q) >= (size_t)p.workgroups * 2 * p.rows * (d + 2) * 4);
+          CHECK(cache_attention_workspace_bytes(n, rows, h[0], h[1], d, q) >= (size_t)p.workgroups * 2 * p.rows * (d + 3) * 4);
         }
   // the axis: as many tiles as 32 bits number, and no more
   CHECK(cache_axis_fits(1, 1, 1, 1, kMaxCachedTokens) && cache_axis_fits(4096, 4096, 28, 4, 1 << 20) && !cache_axis_fits(4096, 4096, 8, 8, kMaxCachedTokens));
