@@ -58,6 +58,7 @@ struct CacheAttnParams {
   int max_len;             // the longest length a row of the table holds
   int hq, hkv, group, causal;
   int workgroups, short_tiles, least_tiles;
+  int row_tiles;           // of a request, by max_q
   float scale_log2;        // softmax_scale * log2(e)
 };
 apbv_status launch_cache_block_attention(const CacheAttnParams& p, int head_dim, hipStream_t stream);      // the parts are left to join

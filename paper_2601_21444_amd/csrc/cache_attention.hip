@@ -24,70 +24,52 @@ enum : int { kHead = 1, kTail = 2, kSpan = 4 };            // what a wave keeps 
 
 // kLse: the log-sum-exp is wanted, and the weights are added up before they are rounded, too: their rounded sum, which the
 // output is divided by, would leave it with errors of 2^-9 over the square root of the number of keys.
-template <int D, int NQ, bool kOnePage, bool kLse>
+// kWhole: a workgroup takes one whole (request, KV head, row tile), its waves a quarter of the keys each, and nothing is left to join.
+template <int D, int NQ, bool kOnePage, bool kLse, bool kWhole>
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(const CacheAttnParams p) {
   using T = Tile<D, 1>;
   constexpr int W = kCacheWaves, R = 16 * NQ;
   // a wave's V tile, later its last piece's O; its first piece's O where it goes on to others (two blocks of rows leave no room
   // for it in LDS: in the workspace)
   constexpr int kWaveLds = T::TILE_BYTES > R * D * 4 ? T::TILE_BYTES : R * D * 4;
-  constexpr bool kHeadsInLds = NQ == 1;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[kHeadsInLds ? 2 : 1][W][kWaveLds];      // [tails, heads]
+  constexpr bool kHeadsInLds = NQ == 1 || kWhole;          // (a whole row tile's last piece is its wave's only one)
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[NQ == 1 && !kWhole ? 2 : 1][W][kWaveLds];      // [tails, heads]
   __shared__ float stat[2][W][3][R];                       // [tails, heads][wave][maximum, row sum, exact row sum]
   __shared__ __attribute__((aligned(16))) int kept[W], place[2][W][4];       // place: first query, rows, KV head, first row
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int li = lane & 15, lg = lane >> 4;
-  Axis<R> axis(p);
-  const uint32_t share = axis.share(p);
-  const int wg = axis.my_share(share);
-  if (wg < 0) return;
-  const uint32_t wg_begin = wg * share;
-  const uint32_t wg_end = share < axis.total - wg_begin ? wg_begin + share : axis.total;
-  // a wave's part of the share
-  const uint32_t wave_share = (wg_end - wg_begin + W - 1) / W;
-  uint32_t pos = wg_begin + wave * wave_share;
-  const uint32_t end = pos + wave_share < wg_end ? pos + wave_share : wg_end;
-  int keeps = 0;
+  int keeps = 0, wg = 0;
 
   // per-lane LDS offsets: V rows as written, and as the A operand of O^T (query_attention.hip)
   constexpr int kPieces = D / 64 * 2;                      // 16-byte chunks of a lane's quarter row
+  auto fv = [](int r) { return T::fv(r) | (r >> 3 & 1); };             // (the bit spreads the writes of sixteen rows over all banks)
   int v_put[kPieces], v_off[T::DBN];
 #pragma unroll
-  for (int x = 0; x < kPieces; ++x) v_put[x] = li * T::ROW_BYTES + (((lg * kPieces + x) ^ T::fv(li)) << 4);
+  for (int x = 0; x < kPieces; ++x) v_put[x] = li * T::ROW_BYTES + (((lg * kPieces + x) ^ fv(li)) << 4);
   {
     const int row = 4 * lg + (li >> 2);
 #pragma unroll
-    for (int d = 0; d < T::DBN; ++d) v_off[d] = row * T::ROW_BYTES + (((2 * d + ((li & 3) >> 1)) ^ T::fv(row)) << 4) + (li & 1) * 8;
+    for (int d = 0; d < T::DBN; ++d) v_off[d] = row * T::ROW_BYTES + (((2 * d + ((li & 3) >> 1)) ^ fv(row)) << 4) + (li & 1) * 8;
   }
   constexpr int kChunks = D / 4;                           // 16-byte chunks of a kept row of O, swizzled by the row
-  float* head_global = p.parts + (int64_t)p.workgroups * 2 * (R * (D + 3)) + (int64_t)wg * W * (R * D);
   unsigned char* vbuf = lds[0][wave];
   const float inv_scale_log2 = 1.0f / p.scale_log2;
 
-  int b = 0;
-  uint32_t begin = 0;
-  if (pos < end) {
-    b = axis.find(p, pos);
-    begin = axis.begin_of(b);
-  }
-#pragma unroll 1
-  while (pos < end) {
-    const Request rq = axis.at(p, b);
-    const int row_tiles = (rq.rows + R - 1) / R;
-    const uint32_t of_request = (uint32_t)(row_tiles * p.hkv) * (uint32_t)rq.tiles;
-    if (pos >= begin + of_request) {                       // (or a request with nothing to do)
-      begin += of_request;
-      ++b;
-      continue;
-    }
-    const uint32_t rel = pos - begin, item = rel / (uint32_t)rq.tiles;
-    const int head = (int)(item / (uint32_t)row_tiles), rt = (int)(item - (uint32_t)head * row_tiles);
-    const int t0 = (int)(rel - item * (uint32_t)rq.tiles);
-    const int t1 = end - pos < (uint32_t)(rq.tiles - t0) ? t0 + (int)(end - pos) : rq.tiles;
-    pos += t1 - t0;
+  auto head_global = [&]() { return p.parts + (int64_t)p.workgroups * 2 * (R * (D + 3)) + (int64_t)wg * W * (R * D); };
+  // Where a wave keeps O of a piece.
+  auto with_kept = [&](int is_head, int w, auto&& f) {
+    if constexpr (kHeadsInLds)
+      f(reinterpret_cast<f32x4*>(lds[kWhole ? 0 : is_head][w]));
+    else if (is_head)
+      f(reinterpret_cast<f32x4*>(head_global() + (int64_t)w * (R * D)));
+    else
+      f(reinterpret_cast<f32x4*>(lds[0][w]));
+  };
 
+  // ---- tiles t0 to t1 - 1 of row tile rt of a request and KV head, by this wave
+  auto piece = [&](const Request& rq, int b, int head, int rt, int t0, int t1) {
     // ---- the row tile's rows: keys each sees, and Q^T fragments (k-step c of lane lg: elements lg * D / 4 + 8 c ...)
     const int r0 = rt * R;
     const int queries = rq.rows / p.group;
@@ -290,18 +272,12 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     } else {
       // (a row tile that ends here but began before is a head; one that goes on, a tail or, of one that began before, a span)
       const int is_head = t1 == rq.tiles ? 1 : 0;
-      auto keep = [&](f32x4* to) {
+      with_kept(is_head, wave, [&](f32x4* to) {
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
           for (int d = 0; d < T::DBN; ++d) to[(16 * nq + li) * kChunks + ((4 * d + lg) ^ li)] = o[d][nq];
-      };
-      if constexpr (kHeadsInLds)
-        keep(reinterpret_cast<f32x4*>(lds[is_head][wave]));
-      else if (is_head)
-        keep(reinterpret_cast<f32x4*>(head_global + (int64_t)wave * (R * D)));
-      else
-        keep(reinterpret_cast<f32x4*>(lds[0][wave]));
+      });
       if (lg == 0) {
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
@@ -318,12 +294,13 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
         place[is_head][wave][3] = r0;
       }
     }
-  }
-  if (lane == 0) kept[wave] = keeps;
-  __syncthreads();
+  };
 
   // ---- the pieces of a row tile that lie in consecutive waves, one chain of them after the other: chain 0 goes on with a row
   // tile that began before this workgroup, chain c begins with the tail of wave c - 1
+  auto put_together = [&]() {
+  if (lane == 0) kept[wave] = keeps;
+  __syncthreads();
   int heads = 0, tails = 0, spans = 0;                     // a bit a wave
 #pragma unroll
   for (int w = 0; w < W; ++w) {
@@ -333,7 +310,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     spans |= (k & kSpan ? 1 : 0) << w;
   }
 #pragma unroll 1
-  for (int chain = 0; chain <= W; ++chain) {
+  for (int chain = kWhole ? 1 : 0; chain <= (kWhole ? 1 : W); ++chain) {
     const int from = chain == 0 ? 0 : chain - 1;
     if (((chain == 0 ? heads | spans : tails) >> from & 1) == 0) continue;
     int to = from;                                         // its last wave
@@ -343,7 +320,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
       else if ((spans >> (to + 1) & 1) == 0) break;        // a wave without a share: the workgroup ends here
       ++to;
     }
-    const bool whole = chain > 0 && ends;
+    const bool whole = kWhole || (chain > 0 && ends);
     const int* at = place[ends && to == from ? 1 : 0][from];
     const int first = at[0], rows = at[1], head = at[2], r0 = at[3];
     const int slot = chain > 0 ? 1 : 0;                    // a part that begins a row tile, or one that goes on with it
@@ -361,17 +338,11 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
         const float weight = __builtin_amdgcn_exp2f(stat[is_head][w][0][row] - m0);
         l = __builtin_fmaf(stat[is_head][w][1][row], weight, l);
         if (kLse) exact = __builtin_fmaf(stat[is_head][w][2][row], weight, exact);
-        auto add = [&](const f32x4* src) {
+        with_kept(is_head, w, [&](const f32x4* src) {
           src += row * kChunks;
           x0 += weight * src[(2 * c) ^ (row & 15)];
           x1 += weight * src[(2 * c + 1) ^ (row & 15)];
-        };
-        if constexpr (kHeadsInLds)
-          add(reinterpret_cast<const f32x4*>(lds[is_head][w]));
-        else if (is_head)
-          add(reinterpret_cast<const f32x4*>(head_global + (int64_t)w * (R * D)));
-        else
-          add(reinterpret_cast<const f32x4*>(lds[0][w]));
+        });
       }
       if (whole) {
         const float inv = l > 0.f ? 1.0f / l : 0.f;
@@ -396,6 +367,64 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
         }
       }
     }
+  }
+  };
+
+  if constexpr (kWhole) {
+    const int head = (int)(blockIdx.x % (uint32_t)p.hkv), rest = (int)(blockIdx.x / (uint32_t)p.hkv), b = rest / p.row_tiles;
+    const int first = p.starts ? scalar_load(p.starts, b) : b * p.each, past = p.starts ? scalar_load(p.starts, b + 1) : (b + 1) * p.each;
+    const Request rq = request_of(p, first, past, scalar_load(p.lengths, b));
+    const int per_wave = (rq.tiles + W - 1) / W, t0 = wave * per_wave, t1 = t0 + per_wave < rq.tiles ? t0 + per_wave : rq.tiles;
+#pragma unroll 1
+    for (int rt = rest % p.row_tiles; rt * R < rq.rows; rt += p.row_tiles) {       // (one, unless max_q is too small)
+      keeps = 0;
+      if (t0 < t1) piece(rq, b, head, rt, t0, t1);
+      put_together();
+      if (rq.tiles == 0)
+        for (int x = threadIdx.x; x < R * (D / 8); x += 64 * W) {
+          const int row = rt * R + x / (D / 8), c = x % (D / 8);
+          if (row >= rq.rows) break;
+          const int i = row / p.group, h = head * p.group + row - i * p.group;
+          *reinterpret_cast<u32x4*>(p.out + ((int64_t)(rq.first + i) * p.hq + h) * D + 8 * c) = u32x4{0u, 0u, 0u, 0u};
+          if (kLse && c == 0) p.lse[(int64_t)h * p.n_rows + rq.first + i] = -INFINITY;
+        }
+      __syncthreads();                                     // LDS is free again
+    }
+  } else {
+    Axis<R> axis(p);
+    const uint32_t share = axis.share(p);
+    wg = axis.my_share(share);
+    if (wg < 0) return;
+    const uint32_t wg_begin = wg * share;
+    const uint32_t wg_end = share < axis.total - wg_begin ? wg_begin + share : axis.total;
+    // a wave's part of the share
+    const uint32_t wave_share = (wg_end - wg_begin + W - 1) / W;
+    uint32_t pos = wg_begin + wave * wave_share;
+    const uint32_t end = pos + wave_share < wg_end ? pos + wave_share : wg_end;
+    int b = 0;
+    uint32_t begin = 0;
+    if (pos < end) {
+      b = axis.find(p, pos);
+      begin = axis.begin_of(b);
+    }
+#pragma unroll 1
+    while (pos < end) {
+      const Request rq = axis.at(p, b);
+      const int row_tiles = (rq.rows + R - 1) / R;
+      const uint32_t of_request = (uint32_t)(row_tiles * p.hkv) * (uint32_t)rq.tiles;
+      if (pos >= begin + of_request) {                     // (or a request with nothing to do)
+        begin += of_request;
+        ++b;
+        continue;
+      }
+      const uint32_t rel = pos - begin, item = rel / (uint32_t)rq.tiles;
+      const int head = (int)(item / (uint32_t)row_tiles), rt = (int)(item - (uint32_t)head * row_tiles);
+      const int t0 = (int)(rel - item * (uint32_t)rq.tiles);
+      const int t1 = end - pos < (uint32_t)(rq.tiles - t0) ? t0 + (int)(end - pos) : rq.tiles;
+      pos += t1 - t0;
+      piece(rq, b, head, rt, t0, t1);
+    }
+    put_together();
   }
 }
 
@@ -511,22 +540,28 @@ void launch_join(Launcher& launch, const CacheAttnParams& p) {
   else
     launch(cache_join_kernel<D, R, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, p);
 }
+template <int D, int NQ, bool kWhole>
+auto few_rows_kernel(const CacheAttnParams& p) {
+  if ((1 << p.cache.page_log2) >= kCacheKeyTile) return p.lse ? cache_attention_kernel<D, NQ, true, true, kWhole> : cache_attention_kernel<D, NQ, true, false, kWhole>;
+  return p.lse ? cache_attention_kernel<D, NQ, false, true, kWhole> : cache_attention_kernel<D, NQ, false, false, kWhole>;
+}
 template <int D, int NQ>
-void launch_few_rows(Launcher& launch, const CacheAttnParams& p) {
-  const bool one_page = (1 << p.cache.page_log2) >= kCacheKeyTile;
-  auto kernel = one_page ? (p.lse ? cache_attention_kernel<D, NQ, true, true> : cache_attention_kernel<D, NQ, true, false>)
-                         : (p.lse ? cache_attention_kernel<D, NQ, false, true> : cache_attention_kernel<D, NQ, false, false>);
-  launch(kernel, dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
+void launch_few_rows(Launcher& launch, const CacheAttnParams& p, bool whole) {
+  if (whole) {
+    launch(few_rows_kernel<D, NQ, true>(p), dim3((unsigned)(p.n_requests * p.hkv * p.row_tiles)), dim3(64 * kCacheWaves), 0, p);
+    return;
+  }
+  launch(few_rows_kernel<D, NQ, false>(p), dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
   launch_join<D, 16 * NQ>(launch, p);
 }
 template <int D>
-apbv_status launch_dim(const CacheAttnParams& p, int rows, hipStream_t stream) {
+apbv_status launch_dim(const CacheAttnParams& p, const CachePlan& plan, hipStream_t stream) {
   if ((int64_t)p.n_rows * p.hq > 0x7fffffff) return APBV_ERR_UNSUPPORTED;
   Launcher launch(stream);
-  if (rows == 16) {
-    launch_few_rows<D, 1>(launch, p);
-  } else if (rows == 32) {
-    launch_few_rows<D, 2>(launch, p);
+  if (plan.rows == 16) {
+    launch_few_rows<D, 1>(launch, p, plan.whole);
+  } else if (plan.rows == 32) {
+    launch_few_rows<D, 2>(launch, p, plan.whole);
   } else {
     const apbv_status st = launch_cache_block_attention(p, D, stream);
     if (st != APBV_OK) return st;
@@ -538,7 +573,7 @@ apbv_status launch_dim(const CacheAttnParams& p, int rows, hipStream_t stream) {
 }  // namespace
 
 apbv_status launch_cache_attention(const CacheAttnParams& p, const CachePlan& plan, int head_dim, hipStream_t stream) {
-  return head_dim == 128 ? launch_dim<128>(p, plan.rows, stream) : launch_dim<64>(p, plan.rows, stream);
+  return head_dim == 128 ? launch_dim<128>(p, plan, stream) : launch_dim<64>(p, plan, stream);
 }
 
 }  // namespace apbv

@@ -117,19 +117,30 @@ struct CachePlan {
   int workgroups;
   int short_tiles;   // where shares would be shorter than this, half as many workgroups share the axis
   int least_tiles;   // a share is not shorter than this
+  int row_tiles;     // of a request
+  bool whole;        // a workgroup for every (request, KV head, row tile)
 };
 // Two workgroups fit a compute unit.  Where each would get but a few tiles, one is given the double: every share costs its start
 // and end and two parts to join (us, 512 / 256 workgroups: one query over 133120 keys, 16 / 2 heads of 128, 8.1 tiles each of
 // 512, 20.3 / 19.3; 256 requests of 65 to 2048 keys, 8 / 2 heads of 64, 9 tiles, 21.6 / 22.9; 64 queries over 16512 keys, 4 tiles,
 // 36 / 34; 64 requests of 512 to 32768 keys, 28 / 4 heads of 128, 56 tiles, 50.6 / 52.0).  Shares of one tile rather than two cost
 // the join more than they save (16000 keys 12.4 / 11.8; 64 queries over 2000 keys 21.6 / 17.4).
-inline CachePlan choose_cache_plan(int hq, int hkv, int d, int64_t max_q) {
+//
+// Where the table holds but a few tiles a request, a workgroup takes a whole (request, KV head, row tile): no axis to plan, no
+// parts, no second launch.  It is alone with its keys, so a table of longer requests, or one of 2048 tokens where there are few,
+// is cut as above (us, cut / whole, one query each, 16 / 2 heads of 128): 1 request of 64 keys 8.2 / 4.5, 700 10.9 / 8.4, 1024 10.9 /
+// 9.6, 2048 11.6 / 13.9; 32 requests of up to 2048 15.4 / 14.2; 256 of up to 1024 24.4 / 15.2, 2048 29.4 / 22.2, 4096 37.0 / 37.1;
+// 256 of 300 to 2048 keys, 5 to 8 queries, 8 / 2 heads of 64 35.7 / 17.4; 64 of 512 to 8192, 28 / 4 heads 29.8 / 42.6.
+inline CachePlan choose_cache_plan(int n_requests, int hq, int hkv, int d, int64_t max_q, int64_t max_len) {
   const int64_t rows = max_q * (hq / hkv);
   CachePlan p;
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kCacheBlockRows;
   p.workgroups = 512;
   p.short_tiles = d == 128 ? 12 : 6;
   p.least_tiles = 2;
+  p.row_tiles = rows <= p.rows ? 1 : (int)((rows + p.rows - 1) / p.rows);
+  const int64_t longest = (max_len + kCacheKeyTile - 1) / kCacheKeyTile;
+  p.whole = p.rows != kCacheBlockRows && (longest <= 20 || (longest <= 32 && (int64_t)n_requests * hkv * p.row_tiles >= 64));
   return p;
 }
 inline size_t cache_part_bytes(int rows, int d) { return (size_t)rows * (size_t)(d + 3) * sizeof(float); }
@@ -137,7 +148,7 @@ inline size_t cache_attention_workspace_bytes(int n_requests, int64_t n_rows, in
   if (check_heads(1, hq, hkv, d) != APBV_OK || n_requests < 1 || n_requests > APBV_CACHE_MAX_REQUESTS || n_rows < 0 || n_rows > kMaxTokens ||
       n_rows * (hq / hkv) > (int64_t)1 << 30 || max_q < 0 || max_q > kMaxTokens)
     return 0;
-  const CachePlan p = choose_cache_plan(hq, hkv, d, max_q);
+  const CachePlan p = choose_cache_plan(n_requests, hq, hkv, d, max_q, 0);
   const size_t heads = p.rows != 32 ? 0 : (size_t)kCacheWaves * p.rows * d * sizeof(float);      // pieces that have no room in LDS
   return align256((size_t)p.workgroups * (2 * cache_part_bytes(p.rows, d) + heads));
 }

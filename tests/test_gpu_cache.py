@@ -1,4 +1,5 @@
 """The 4-bit key/value cache on the GPU against the fp64 oracle: rows and tables exactly, attention within bounds derived below."""
+import itertools
 import math
 
 import numpy as np
@@ -252,14 +253,20 @@ class Batch:
     def lengths(self):
         return dev_int([k for _, k in self.requests])
 
-    def run(self, causal=True, starts=True, **kw):
+    def run(self, causal=True, starts=True, wide=False, **kw):
+        """wide: the table has room for longer requests, so that keys are cut among workgroups and parts joined."""
         out = torch.full((self.rows, self.hq, self.d), 77.0, dtype=torch.bfloat16, device="cuda")
         lse = torch.full((self.hq, self.rows), 77.0, device="cuda")
         if starts:
             kw.setdefault("q_starts", dev_int(self.starts))
             kw.setdefault("max_q", max(n for n, _ in self.requests))
-        apbv.apbv_cache_attention(self.q, self.cache, dev_int(self.table.tolist()), self.lengths(), self.scale, causal=causal, out=out, lse_out=lse, **kw)
+        table = np.concatenate((self.table, np.full((len(self.requests), 5000 // self.page), -1)), 1) if wide else self.table
+        apbv.apbv_cache_attention(self.q, self.cache, dev_int(table.tolist()), self.lengths(), self.scale, causal=causal, out=out, lse_out=lse, **kw)
         torch.cuda.synchronize()
+        if "max_q" in kw and not causal:                    # without the log-sum-exp: the same outputs
+            again = torch.full_like(out, 77.0)
+            apbv.apbv_cache_attention(self.q, self.cache, dev_int(table.tolist()), self.lengths(), self.scale, causal=causal, out=again, **kw)
+            assert torch.equal(out.view(torch.int16), again.view(torch.int16))
         return out, lse
 
     def check(self, out, lse, causal=True, what=""):
@@ -288,20 +295,21 @@ SHAPES = [
 ]
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("case", range(len(SHAPES)))
-def test_attention_matches_the_oracle(case, causal):
+def test_attention_matches_the_oracle(case, causal, wide):
     hq, hkv, d, page, requests = SHAPES[case]
-    print("attention", SHAPES[case], causal, flush=True)
+    print("attention", SHAPES[case], causal, wide, flush=True)
     x = Batch(np.random.default_rng((5, case)), hq, hkv, d, page, requests, lead=case % 3, tail=case % 2 * 3)
-    out, lse = x.run(causal)
+    out, lse = x.run(causal, wide=wide)
     x.check(out, lse, causal, f"case {case} causal={causal}")
-    again, lse_again = x.run(causal)
+    again, lse_again = x.run(causal, wide=wide)
     assert torch.equal(out.view(torch.int16), again.view(torch.int16)) and torch.equal(lse, lse_again)
     # max_q changes how the work is cut, not what is computed
-    more, lse_more = x.run(causal, max_q=x.rows + 1)
+    more, lse_more = x.run(causal, wide=wide, max_q=x.rows + 1)
     x.check(more, lse_more, causal, f"case {case} causal={causal}, a large max_q")
-    fewer, lse_fewer = x.run(causal, max_q=0)
+    fewer, lse_fewer = x.run(causal, wide=wide, max_q=0)
     x.check(fewer, lse_fewer, causal, f"case {case} causal={causal}, max_q too small")
 
 
@@ -309,8 +317,9 @@ def test_attention_matches_the_oracle(case, causal):
 def test_attention_of_equal_blocks_without_starts(queries):
     x = Batch(np.random.default_rng((6, queries)), 8, 2, 128, 32, [(queries, 64 * i + 41) for i in range(5)])
     print("equal blocks", queries, flush=True)
-    out, lse = x.run(starts=False)
-    x.check(out, lse, True, f"{queries} each")
+    for wide in (False, True):
+        out, lse = x.run(starts=False, wide=wide)
+        x.check(out, lse, True, f"{queries} each")
 
 
 def test_many_requests():
@@ -322,6 +331,10 @@ def test_many_requests():
     print("333 requests", flush=True)
     out, lse = x.run()
     x.check(out, lse, True, "many")
+    x.requests[200], x.k[200], x.v[200] = (1, 1000), x.k[200][:1000], x.v[200][:1000]
+    x.table = x.table[:, :63]                               # a short table
+    out, lse = x.run()
+    x.check(out, lse, True, "many, short")
 
 
 def test_peaked_logits_and_growing_keys():
@@ -330,8 +343,9 @@ def test_peaked_logits_and_growing_keys():
         x = Batch(np.random.default_rng((8, int(factor))), 8, 1, 128, 64, [(1, 1500), (5, 600)], k_scale=factor)
         x.qv *= 0.25
         x.q = (x.q.float() * 0.25).bfloat16()
-        out, lse = x.run()
-        x.check(out, lse, True, f"keys of scale {factor}")
+        for wide in (False, True):
+            out, lse = x.run(wide=wide)
+            x.check(out, lse, True, f"keys of scale {factor}")
 
 
 def test_keys_on_bad_pages_are_not_there():
@@ -341,8 +355,8 @@ def test_keys_on_bad_pages_are_not_there():
     gone = [(0, 0, -1), (0, 5, n_pages), (1, 15, -2 ** 31), (1, 3, 2 ** 31 - 1), (2, 0, n_pages + 7)]
     for b, i, page in gone:
         x.table[b, i] = page
-    out, lse = x.run(causal=False)
-    for b, (n, keys) in enumerate(x.requests):
+    for wide, (b, (n, keys)) in itertools.product((False, True), enumerate(x.requests)):
+        out, lse = x.run(causal=False, wide=wide)
         keep = np.ones(keys, bool)
         for bb, i, _ in gone:
             if bb == b:
