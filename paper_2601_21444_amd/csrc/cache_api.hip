@@ -70,7 +70,7 @@ apbv_status apbv_cache_attention(const apbv_cache* cache, int n_requests, int n_
   const apbv_status st = validate_cache_attention(cache, n_requests, n_q_heads, n_kv_heads, head_dim, q, block_table, table_stride, max_blocks,
                                                   lengths, q_starts, max_q, softmax_scale, out, lse_out);
   if (st != APBV_OK || q.tokens == 0) return st;
-  const CachePlan plan = choose_cache_plan(n_requests, n_q_heads, n_kv_heads, head_dim, max_q, max_blocks * cache->page_size);
+  const CachePlan plan = choose_cache_plan(n_requests, n_q_heads, n_kv_heads, head_dim, q.tokens, max_q, max_blocks * cache->page_size);
   const size_t need = cache_attention_workspace_bytes(n_requests, q.tokens, n_q_heads, n_kv_heads, head_dim, max_q);
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < need) return APBV_ERR_WORKSPACE;
   CacheAttnParams p;

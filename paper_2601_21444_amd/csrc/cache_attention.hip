@@ -533,10 +533,10 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
 }
 
 template <int D, int R>
-void launch_join(Launcher& launch, const CacheAttnParams& p) {
+void launch_join(Launcher& launch, const CacheAttnParams& p, int waves) {
   const int64_t rows = (int64_t)p.n_rows * p.hq;
-  if (rows <= kCacheJoinRows)
-    launch(cache_join_kernel<D, R, 16>, dim3((unsigned)rows), dim3(1024), 0, p);
+  if (waves == 4)
+    launch(cache_join_kernel<D, R, 4>, dim3((unsigned)rows), dim3(256), 0, p);
   else
     launch(cache_join_kernel<D, R, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, p);
 }
@@ -546,26 +546,26 @@ auto few_rows_kernel(const CacheAttnParams& p) {
   return p.lse ? cache_attention_kernel<D, NQ, false, true, kWhole> : cache_attention_kernel<D, NQ, false, false, kWhole>;
 }
 template <int D, int NQ>
-void launch_few_rows(Launcher& launch, const CacheAttnParams& p, bool whole) {
-  if (whole) {
+void launch_few_rows(Launcher& launch, const CacheAttnParams& p, const CachePlan& plan) {
+  if (plan.whole) {
     launch(few_rows_kernel<D, NQ, true>(p), dim3((unsigned)(p.n_requests * p.hkv * p.row_tiles)), dim3(64 * kCacheWaves), 0, p);
     return;
   }
   launch(few_rows_kernel<D, NQ, false>(p), dim3((unsigned)p.workgroups), dim3(64 * kCacheWaves), 0, p);
-  launch_join<D, 16 * NQ>(launch, p);
+  launch_join<D, 16 * NQ>(launch, p, plan.join_waves);
 }
 template <int D>
 apbv_status launch_dim(const CacheAttnParams& p, const CachePlan& plan, hipStream_t stream) {
   if ((int64_t)p.n_rows * p.hq > 0x7fffffff) return APBV_ERR_UNSUPPORTED;
   Launcher launch(stream);
   if (plan.rows == 16) {
-    launch_few_rows<D, 1>(launch, p, plan.whole);
+    launch_few_rows<D, 1>(launch, p, plan);
   } else if (plan.rows == 32) {
-    launch_few_rows<D, 2>(launch, p, plan.whole);
+    launch_few_rows<D, 2>(launch, p, plan);
   } else {
     const apbv_status st = launch_cache_block_attention(p, D, stream);
     if (st != APBV_OK) return st;
-    launch_join<D, kCacheBlockRows>(launch, p);
+    launch_join<D, kCacheBlockRows>(launch, p, plan.join_waves);
   }
   return launch.status();
 }

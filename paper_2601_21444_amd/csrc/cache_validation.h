@@ -111,7 +111,6 @@ inline apbv_status validate_cache_attention(const apbv_cache* cache, int n_reque
 // (request, head, row tile) leaves a part of it in the workspace: at most two a workgroup.
 constexpr int kCacheBlockRows = 128;        // rows of a row tile of query blocks and chunks
 constexpr int kCacheWaves = 4;              // waves of a workgroup
-constexpr int kCacheJoinRows = 512;         // rows (query x head) up to which several waves join the parts of one
 struct CachePlan {
   int rows;          // query rows (query x head of the KV group) of a row tile
   int workgroups;
@@ -119,6 +118,7 @@ struct CachePlan {
   int least_tiles;   // a share is not shorter than this
   int row_tiles;     // of a request
   bool whole;        // a workgroup for every (request, KV head, row tile)
+  int join_waves;    // waves that join the parts of a row: 1 or 4
 };
 // Two workgroups fit a compute unit.  Where each would get but a few tiles, one is given the double: every share costs its start
 // and end and two parts to join (us, 512 / 256 workgroups: one query over 133120 keys, 16 / 2 heads of 128, 8.1 tiles each of
@@ -131,7 +131,12 @@ struct CachePlan {
 // is cut as above (us, cut / whole, one query each, 16 / 2 heads of 128): 1 request of 64 keys 8.2 / 4.5, 700 10.9 / 8.4, 1024 10.9 /
 // 9.6, 2048 11.6 / 13.9; 32 requests of up to 2048 15.4 / 14.2; 256 of up to 1024 24.4 / 15.2, 2048 29.4 / 22.2, 4096 37.0 / 37.1;
 // 256 of 300 to 2048 keys, 5 to 8 queries, 8 / 2 heads of 64 35.7 / 17.4; 64 of 512 to 8192, 28 / 4 heads 29.8 / 42.6.
-inline CachePlan choose_cache_plan(int n_requests, int hq, int hkv, int d, int64_t max_q, int64_t max_len) {
+//
+// The second launch takes a wave per row of the output, or four where the rows are few and have many parts (us for the call, one
+// wave / four: one query over 133120 keys, 16 / 2 heads of 128 24.8 / 19.6, 17 queries over 10000, 28 / 4 heads 24.4 / 22.7, 64
+// queries over 16512, 16 / 2 heads 32.8 / 32.3; 4 x 64 queries, 8 / 2 heads of 64 19.6 / 22.7, 64 requests of one query, 28 / 4
+// heads 51.6 / 55.1).
+inline CachePlan choose_cache_plan(int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q, int64_t max_len) {
   const int64_t rows = max_q * (hq / hkv);
   CachePlan p;
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kCacheBlockRows;
@@ -141,6 +146,8 @@ inline CachePlan choose_cache_plan(int n_requests, int hq, int hkv, int d, int64
   p.row_tiles = rows <= p.rows ? 1 : (int)((rows + p.rows - 1) / p.rows);
   const int64_t longest = (max_len + kCacheKeyTile - 1) / kCacheKeyTile;
   p.whole = p.rows != kCacheBlockRows && (longest <= 20 || (longest <= 32 && (int64_t)n_requests * hkv * p.row_tiles >= 64));
+  const int64_t parts = p.workgroups / ((int64_t)n_requests * hkv * p.row_tiles) + 1;      // of a row, if the requests are alike
+  p.join_waves = parts > 8 && n_rows * hq <= 1024 ? 4 : 1;
   return p;
 }
 inline size_t cache_part_bytes(int rows, int d) { return (size_t)rows * (size_t)(d + 3) * sizeof(float); }
@@ -148,7 +155,7 @@ inline size_t cache_attention_workspace_bytes(int n_requests, int64_t n_rows, in
   if (check_heads(1, hq, hkv, d) != APBV_OK || n_requests < 1 || n_requests > APBV_CACHE_MAX_REQUESTS || n_rows < 0 || n_rows > kMaxTokens ||
       n_rows * (hq / hkv) > (int64_t)1 << 30 || max_q < 0 || max_q > kMaxTokens)
     return 0;
-  const CachePlan p = choose_cache_plan(n_requests, hq, hkv, d, max_q, 0);
+  const CachePlan p = choose_cache_plan(n_requests, hq, hkv, d, n_rows, max_q, 0);
   const size_t heads = p.rows != 32 ? 0 : (size_t)kCacheWaves * p.rows * d * sizeof(float);      // pieces that have no room in LDS
   return align256((size_t)p.workgroups * (2 * cache_part_bytes(p.rows, d) + heads));
 }
