@@ -60,6 +60,7 @@ struct CacheAttnParams {
   int workgroups, short_tiles, least_tiles;
   int row_tiles;           // of a request, by max_q
   float scale_log2;        // softmax_scale * log2(e)
+  double per_group;        // 1 / group
 };
 apbv_status launch_cache_block_attention(const CacheAttnParams& p, int head_dim, hipStream_t stream);      // the parts are left to join
 apbv_status launch_cache_attention(const CacheAttnParams& p, const CachePlan& plan, int head_dim, hipStream_t stream);

@@ -96,6 +96,7 @@ apbv_status apbv_cache_attention(const apbv_cache* cache, int n_requests, int n_
   p.least_tiles = plan.least_tiles;
   p.row_tiles = plan.row_tiles;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
+  p.per_group = 1.0 / p.group;
   return launch_cache_attention(p, plan, head_dim, static_cast<hipStream_t>(hip_stream));
 }
 

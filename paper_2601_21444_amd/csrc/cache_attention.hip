@@ -72,22 +72,22 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
   auto piece = [&](const Request& rq, int b, int head, int rt, int t0, int t1) {
     // ---- the row tile's rows: keys each sees, and Q^T fragments (k-step c of lane lg: elements lg * D / 4 + 8 c ...)
     const int r0 = rt * R;
-    const int queries = rq.rows / p.group;
+    const int queries = query_of(p, rq.rows);
     bf16x8 qf[T::KSD][NQ];
     int jlast[NQ];
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
       const int r = r0 + 16 * nq + li < rq.rows ? r0 + 16 * nq + li : rq.rows - 1;
-      const int i = r / p.group;
+      const int i = query_of(p, r);
       jlast[nq] = p.causal ? rq.len - queries + i : rq.len - 1;
-      const bf16_t* qrow = p.q.ptr + (int64_t)(rq.first + i) * p.q.st + (int64_t)(head * p.group + r % p.group) * p.q.sh + lg * (D / 4);
+      const bf16_t* qrow = p.q.ptr + (int64_t)(rq.first + i) * p.q.st + (int64_t)(head * p.group + r - i * p.group) * p.q.sh + lg * (D / 4);
 #pragma unroll
       for (int c = 0; c < T::KSD; ++c) qf[c][nq] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + 8 * c));
     }
     // keys that every row sees, keys that some row sees
-    const int all = p.causal ? rq.len - queries + r0 / p.group + 1 : rq.len;
+    const int all = p.causal ? rq.len - queries + query_of(p, r0) + 1 : rq.len;
     const int last_row = r0 + R < rq.rows ? r0 + R - 1 : rq.rows - 1;
-    const int some = p.causal ? rq.len - queries + last_row / p.group + 1 : rq.len;
+    const int some = p.causal ? rq.len - queries + query_of(p, last_row) + 1 : rq.len;
     const int t_end = some <= 0 ? 0 : (t1 * kCacheKeyTile < some ? t1 : (some + kCacheKeyTile - 1) / kCacheKeyTile);
 
     f32x4 o[T::DBN][NQ];
@@ -217,8 +217,9 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     int t = t0;
     if (t < t_end) {
 #pragma unroll
+      for (int a = 0; a < kAhead; ++a) find(at[a], t + a);
+#pragma unroll
       for (int a = 0; a < kAhead; ++a) {
-        find(at[a], t + a);
         load_k(at[a], kc[a]);
         load_v(at[a], vc[a]);
       }
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
       for (int nq = 0; nq < NQ; ++nq) {
         const int row = r0 + 16 * nq + li;
         if (row >= rq.rows) continue;
-        const int i = row / p.group, h = head * p.group + row % p.group;
+        const int i = query_of(p, row), h = head * p.group + row - i * p.group;
         const float inv = l_tot[nq] > 0.f ? 1.0f / l_tot[nq] : 0.f;
         bf16_t* dst = p.out + ((int64_t)(rq.first + i) * p.hq + h) * D + 4 * lg;
 #pragma unroll
@@ -329,13 +330,21 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     for (int x = threadIdx.x; x < R * (D / 8); x += 64 * W) {
       const int row = x / (D / 8), c = x % (D / 8);
       if (r0 + row >= rows) break;
-      float m = -INFINITY, l = 0.f, exact = 0.f;
-      for (int w = from; w <= to; ++w) m = fmaxf(m, stat[w == to && ends ? 1 : 0][w][0][row]);
+      // (all waves' statistics, then all waves' rows, are read at once, those of others than the chain's left out)
+      float m_of[W], l = 0.f, exact = 0.f, m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        m_of[w] = stat[w == to && ends ? 1 : 0][w][0][row];
+        m_of[w] = w >= from && w <= to ? m_of[w] : -INFINITY;
+        m = fmaxf(m, m_of[w]);
+      }
       const float m0 = m > -INFINITY ? m : 0.f;
       f32x4 x0 = {0.f, 0.f, 0.f, 0.f}, x1 = {0.f, 0.f, 0.f, 0.f};
-      for (int w = from; w <= to; ++w) {
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        if (w < from || w > to) continue;
         const int is_head = w == to && ends ? 1 : 0;
-        const float weight = __builtin_amdgcn_exp2f(stat[is_head][w][0][row] - m0);
+        const float weight = __builtin_amdgcn_exp2f(m_of[w] - m0);
         l = __builtin_fmaf(stat[is_head][w][1][row], weight, l);
         if (kLse) exact = __builtin_fmaf(stat[is_head][w][2][row], weight, exact);
         with_kept(is_head, w, [&](const f32x4* src) {
@@ -353,7 +362,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
         y.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x0.z, x0.w}), bf16x2));
         y.z = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x1.x, x1.y}), bf16x2));
         y.w = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x1.z, x1.w}), bf16x2));
-        const int i = (r0 + row) / p.group, h = head * p.group + (r0 + row) % p.group;
+        const int i = query_of(p, r0 + row), h = head * p.group + r0 + row - i * p.group;
         *reinterpret_cast<u32x4*>(p.out + ((int64_t)(first + i) * p.hq + h) * D + 8 * c) = y;
         if (kLse && c == 0) p.lse[(int64_t)h * p.n_rows + first + i] = log_sum(m, exact);
       } else {
@@ -384,7 +393,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
         for (int x = threadIdx.x; x < R * (D / 8); x += 64 * W) {
           const int row = rt * R + x / (D / 8), c = x % (D / 8);
           if (row >= rq.rows) break;
-          const int i = row / p.group, h = head * p.group + row - i * p.group;
+          const int i = query_of(p, row), h = head * p.group + row - i * p.group;
           *reinterpret_cast<u32x4*>(p.out + ((int64_t)(rq.first + i) * p.hq + h) * D + 8 * c) = u32x4{0u, 0u, 0u, 0u};
           if (kLse && c == 0) p.lse[(int64_t)h * p.n_rows + rq.first + i] = -INFINITY;
         }

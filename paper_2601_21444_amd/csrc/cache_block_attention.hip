@@ -92,13 +92,13 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_ker
 
     // ---- keys that every row of the wave sees, that this lane's row sees last, that some row of the workgroup sees
     const int r_tile = rt * R, rw = r_tile + 32 * wave;
-    const int queries = rq.rows / p.group;
-    const int row = rw + c < rq.rows ? rw + c : rq.rows - 1, qi = row / p.group;
+    const int queries = query_of(p, rq.rows);
+    const int row = rw + c < rq.rows ? rw + c : rq.rows - 1, qi = query_of(p, row);
     const int jlast = p.causal ? rq.len - queries + qi : rq.len - 1;
     const int r_first = rw < rq.rows ? rw : rq.rows - 1;
-    const int all = p.causal ? rq.len - queries + r_first / p.group + 1 : rq.len;
+    const int all = p.causal ? rq.len - queries + query_of(p, r_first) + 1 : rq.len;
     const int r_last = r_tile + R < rq.rows ? r_tile + R - 1 : rq.rows - 1;
-    const int some = p.causal ? rq.len - queries + r_last / p.group + 1 : rq.len;
+    const int some = p.causal ? rq.len - queries + query_of(p, r_last) + 1 : rq.len;
     const int t_end = some <= 0 ? 0 : (t1 * kCacheKeyTile < some ? t1 : (some + kCacheKeyTile - 1) / kCacheKeyTile);
 
     // ---- this wave's 16 keys of a tile (past the last tile: of the last one, again).  The page is looked up a tile before its

@@ -10,6 +10,10 @@ namespace {
 #define APBV_CONST(T) const __attribute__((address_space(4))) T*     // read through the scalar cache
 __device__ __forceinline__ int scalar_load(const int32_t* p, int64_t i) { return ((APBV_CONST(int32_t))p)[i]; }
 
+// The query that a row (query x head of the group, below 2^30) is of.  (row + 1/2) / group is no nearer to a whole number than 1 /
+// (2 group), the double's error is below 2^-20: three instructions where the division of integers has twenty.
+__device__ __forceinline__ int query_of(const CacheAttnParams& p, int row) { return (int)(((double)row + 0.5) * p.per_group); }
+
 struct Request {
   int first, rows, len;      // first query, rows (query x head of the group), keys
   int tiles;                 // 64-key tiles of each of its row tiles; 0: none
