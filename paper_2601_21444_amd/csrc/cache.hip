@@ -345,21 +345,25 @@ __global__ __launch_bounds__(256) void cache_slots_kernel(const CacheMapParams p
   for (int b = threadIdx.x; b <= n; b += 256) first[b] = p.starts_out[b];
   __syncthreads();
   const int total = first[n];
+  // (each step for all of a thread's tokens before the next: three waits for memory, not three a token)
+  int t[kSlotsPerThread], owner_of[kSlotsPerThread], now[kSlotsPerThread], asked[kSlotsPerThread], slot[kSlotsPerThread];
 #pragma unroll
   for (int u = 0; u < kSlotsPerThread; ++u) {
-    const int t = (blockIdx.x * kSlotsPerThread + u) * 256 + threadIdx.x;
-    if (t >= p.max_new) break;
-    int slot = -1;
-    if (t < total) {
-      const int b = owner(first, n, t);
-      const int now = p.lengths_out[b];
-      if (now == p.new_lengths[b]) {
-        const int pos = now - (first[b + 1] - t);
-        slot = slot_of(p.table[(int64_t)b * p.table_stride + (pos >> p.page_log2)], pos, p.page_log2);
-      }
-    }
-    p.slots_out[t] = slot;
+    t[u] = (blockIdx.x * kSlotsPerThread + u) * 256 + threadIdx.x;
+    owner_of[u] = t[u] < total ? owner(first, n, t[u]) : 0;
+    now[u] = p.lengths_out[owner_of[u]];
+    asked[u] = p.new_lengths[owner_of[u]];
   }
+#pragma unroll
+  for (int u = 0; u < kSlotsPerThread; ++u) {
+    const bool granted = t[u] < total && now[u] == asked[u];
+    const int pos = granted ? now[u] - (first[owner_of[u] + 1] - t[u]) : 0;
+    now[u] = pos;
+    slot[u] = granted ? p.table[(int64_t)owner_of[u] * p.table_stride + (pos >> p.page_log2)] : -1;
+  }
+#pragma unroll
+  for (int u = 0; u < kSlotsPerThread; ++u)
+    if (t[u] < p.max_new) p.slots_out[t[u]] = slot_of(slot[u], now[u], p.page_log2);
 }
 
 }  // namespace
