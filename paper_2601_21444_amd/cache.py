@@ -97,9 +97,13 @@ def _check_table(t: torch.Tensor, n: int, device: torch.device):
     return t.stride(0), t.shape[1]
 
 
-def _rows_device(t: torch.Tensor, name: str) -> torch.device:
+def _rows_device(t: torch.Tensor, name: str, stream: Optional[torch.cuda.Stream]) -> torch.device:
+    """The device of a call: a GPU, and that of the stream the call is enqueued on."""
     if not t.is_cuda:
         raise ValueError(f"{name}: must live on a GPU")
+    on = torch.cuda.current_device() if stream is None else stream.device.index
+    if t.device.index != on:
+        raise ValueError(f"{name}: lives on {t.device}, the stream of the call on cuda:{on}")
     return t.device
 
 
@@ -118,7 +122,7 @@ def apbv_cache_map(old_lengths: torch.Tensor, new_lengths: torch.Tensor, block_t
             if st != 0:
                 raise ApbvError(st, "apbv_cache_map")
             return lengths_out, starts_out, slots_out, free_count_out
-    dev = _rows_device(old_lengths, "old_lengths")
+    dev = _rows_device(old_lengths, "old_lengths", stream)
     n, max_new = old_lengths.numel(), operator.index(max_new_tokens)
     _check_ints(old_lengths, "old_lengths", (n,), dev)
     _check_ints(new_lengths, "new_lengths", (n,), dev)
@@ -155,7 +159,7 @@ def apbv_cache_store(cache: ApbvCache, k: torch.Tensor, v: torch.Tensor, slots: 
             if st != 0:
                 raise ApbvError(st, "apbv_cache_store")
             return cache
-    dev = _rows_device(k, "k")
+    dev = _rows_device(k, "k", stream)
     view, heads, d = _cache_view(cache, dev)
     views = []
     for name, t in (("k", k), ("v", v)):
@@ -180,7 +184,7 @@ def apbv_cache_load(cache: ApbvCache, slots: torch.Tensor, *, k_out: Optional[to
             if st != 0:
                 raise ApbvError(st, "apbv_cache_load")
             return k_out, v_out
-    dev = _rows_device(slots, "slots")
+    dev = _rows_device(slots, "slots", stream)
     view, heads, d = _cache_view(cache, dev)
     n = slots.numel()
     _check_ints(slots, "slots", (n,), dev)
@@ -215,7 +219,7 @@ def apbv_cache_attention(q: torch.Tensor, cache: ApbvCache, block_table: torch.T
             if st != 0:
                 raise ApbvError(st, "apbv_cache_attention")
             return (out, lse_out) if return_lse else out
-    dev = _rows_device(q, "q")
+    dev = _rows_device(q, "q", stream)
     view, heads, d = _cache_view(cache, dev)
     if q.dim() != 3 or q.shape[2] != d:
         raise ValueError(f"q: expected [rows, heads, {d}]")

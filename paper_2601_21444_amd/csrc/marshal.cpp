@@ -88,15 +88,19 @@ bool whole(PyObject* o, int64_t& x) {
   return overflow == 0;
 }
 
-// The current device's current stream; false if CUDA is not initialised in this process, or with what was raised (by a signal's
-// handler, say: these functions run Python code).
-bool current_stream(void*& stream) {
+// The current device's current stream; false if CUDA is not initialised in this process, if that device is not `on`, or with what
+// was raised (by a signal's handler, say: these functions run Python code).
+bool current_stream(void*& stream, const c10::Device* on = nullptr) {
   PyObject* ok = PyObject_CallNoArgs(g_is_initialized);
   const bool ready = ok == Py_True;
   Py_XDECREF(ok);
   if (!ready) return false;
   PyObject* dev = PyObject_CallNoArgs(g_current_device);
   if (dev == nullptr) return false;
+  if (on != nullptr && PyLong_AsLong(dev) != on->index()) {
+    Py_DECREF(dev);
+    return false;
+  }
   PyObject* raw = PyObject_CallOneArg(g_raw_stream, dev);
   Py_DECREF(dev);
   if (raw == nullptr) return false;
@@ -336,7 +340,7 @@ PyObject* cache_map(PyObject*, PyObject* const* a, Py_ssize_t count) {
     for (int i = 7; i < 11; ++i)
       if (a[i] == Py_None) return false;
     if (!buffer(a[7], at::kInt, n, device, false, lengths) || !buffer(a[8], at::kInt, n + 1, device, false, starts) ||
-        !buffer(a[9], at::kInt, max_new, device, false, slots) || !buffer(a[10], at::kInt, 1, device, false, left) || !current_stream(stream))
+        !buffer(a[9], at::kInt, max_new, device, false, slots) || !buffer(a[10], at::kInt, 1, device, false, left) || !current_stream(stream, &device))
       return false;
     Py_BEGIN_ALLOW_THREADS
     status = apbv_cache_map(to_int(n), to_int(page), blocks, old_l, new_l, table, stride, capacity > 0 ? free_pages : nullptr, capacity, free_count, max_new,
@@ -357,7 +361,7 @@ PyObject* cache_store(PyObject*, PyObject* const* a, Py_ssize_t count) {
     void* stream;
     if (!cache_of(a[0], c) || !view_of(a[1], k, 3) || !view_of(a[2], v, 3) || k.device != c.device || v.device != c.device) return false;
     if (k.heads != c.heads || v.heads != c.heads || k.d != c.d || v.d != c.d || v.tokens != k.tokens) return false;
-    if (!ints(a[3], k.tokens, c.device, slots) || !current_stream(stream)) return false;
+    if (!ints(a[3], k.tokens, c.device, slots) || !current_stream(stream, &c.device)) return false;
     Py_BEGIN_ALLOW_THREADS
     status = apbv_cache_store(&c.view, to_int(c.heads), to_int(c.d), k.view, v.view, k.tokens > 0 ? slots : nullptr, stream);
     Py_END_ALLOW_THREADS
@@ -374,7 +378,7 @@ PyObject* cache_load(PyObject*, PyObject* const* a, Py_ssize_t count) {
     int32_t* slots;
     void *k, *v, *stream;
     if (!cache_of(a[0], c) || !ints(a[1], n, c.device, slots) || a[2] == Py_None || a[3] == Py_None) return false;
-    if (!buffer(a[2], at::kBFloat16, n * c.heads * c.d, c.device, false, k) || !buffer(a[3], at::kBFloat16, n * c.heads * c.d, c.device, false, v) || !current_stream(stream))
+    if (!buffer(a[2], at::kBFloat16, n * c.heads * c.d, c.device, false, k) || !buffer(a[3], at::kBFloat16, n * c.heads * c.d, c.device, false, v) || !current_stream(stream, &c.device))
       return false;
     if (n == 0) slots = nullptr, k = v = nullptr;
     Py_BEGIN_ALLOW_THREADS
@@ -405,7 +409,7 @@ PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
     else if (!whole(a[6], max_q))
       return false;
     if (a[8] == Py_None || a[10] == Py_None || !buffer(a[8], at::kBFloat16, q.tokens * q.heads * q.d, c.device, false, out) ||
-        !buffer(a[9], at::kFloat, q.heads * q.tokens, c.device, true, lse) || !buffer(a[10], at::kByte, 0, c.device, false, ws, &ws_bytes) || !current_stream(stream))
+        !buffer(a[9], at::kFloat, q.heads * q.tokens, c.device, true, lse) || !buffer(a[10], at::kByte, 0, c.device, false, ws, &ws_bytes) || !current_stream(stream, &c.device))
       return false;
     if (q.tokens == 0) out = nullptr;
     const int causal = a[7] == Py_True;

@@ -183,3 +183,20 @@ def test_binding_refuses_what_does_not_fit():
         apbv.apbv_cache_load(c, i(3))
     with pytest.raises(ValueError, match="must live on a GPU"):
         apbv.apbv_cache_map(i(3), i(3), i(3, 2), i(5), i(1), 16, 4)
+
+
+class Elsewhere:
+    """What the binding asks of a tensor's place: a second GPU's."""
+    is_cuda, device = True, torch.device("cuda", 1)
+
+
+def test_tensors_of_another_device_than_the_streams_are_refused(monkeypatch):
+    from paper_2601_21444_amd import cache as module
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="the stream of the call on cuda:0"):
+        module._rows_device(Elsewhere, "q", None)
+    stream = type("Stream", (), {"device": torch.device("cuda", 0)})
+    with pytest.raises(ValueError, match="the stream of the call on cuda:0"):
+        module._rows_device(Elsewhere, "q", stream)
+    stream.device = torch.device("cuda", 1)
+    assert module._rows_device(Elsewhere, "q", stream) == torch.device("cuda", 1)
