@@ -14,7 +14,6 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding
-from . import binding
 from .binding import ApbvCacheStruct, ApbvError, _check_buffer, _stream_ptr, load_library, tensor_view
 
 CACHE_MAX_REQUESTS = 4096      # APBV_CACHE_MAX_REQUESTS of include/apbv_cache.h

@@ -137,7 +137,7 @@ struct CachePlan {
 // queries over 16512, 16 / 2 heads 32.8 / 32.3; 4 x 64 queries, 8 / 2 heads of 64 19.6 / 22.7, 64 requests of one query, 28 / 4
 // heads 51.6 / 55.1).
 inline CachePlan choose_cache_plan(int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q, int64_t max_len) {
-  const int64_t rows = max_q * (hq / hkv);
+  const int64_t rows = (max_q < n_rows ? max_q : n_rows) * (hq / hkv);      // at most 2^30
   CachePlan p;
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kCacheBlockRows;
   p.workgroups = 512;

@@ -127,6 +127,13 @@ def test_attention_workspace_query():
     assert ws(2, 6, 8, 2, 64, 1) % 256 == 0
 
 
+def test_a_request_has_no_more_rows_than_there_are():
+    # (2^39 rows by max_q alone: a multiple of 2^32 row tiles)
+    ws = apbv.apbv_cache_attention_workspace_bytes
+    assert ws(1, 1, 32768, 1, 64, 1 << 24) == ws(1, 1, 32768, 1, 64, 1) > 0
+    assert ws(2, 6, 8, 2, 128, 1 << 24) == ws(2, 6, 8, 2, 128, 6)
+
+
 def test_store_and_load_refuse_bad_arguments_without_launching():
     lib = apbv.load_library()
 
