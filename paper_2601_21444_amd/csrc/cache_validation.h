@@ -47,7 +47,7 @@ inline apbv_status validate_cache_map(int n_requests, int page_size, int64_t max
   if (!valid_page_size(page_size)) return APBV_ERR_UNSUPPORTED;
   const apbv_status st = check_table(n_requests, page_size, table, table_stride, max_blocks);
   if (st != APBV_OK) return st;
-  if (free_capacity < 0 || free_capacity > kMaxSlots || max_new_tokens < 0 || max_new_tokens > kMaxTokens) return APBV_ERR_SHAPE;
+  if (free_capacity < 0 || free_capacity > kMaxSlots / page_size || max_new_tokens < 0 || max_new_tokens > kMaxTokens) return APBV_ERR_SHAPE;
   if (old_lengths == nullptr || new_lengths == nullptr || free_count == nullptr || lengths_out == nullptr || starts_out == nullptr ||
       free_count_out == nullptr || (free_pages == nullptr && free_capacity > 0) || (slots_out == nullptr && max_new_tokens > 0))
     return APBV_ERR_NULL;

@@ -165,6 +165,7 @@ def test_map_refuses_bad_arguments_without_launching():
     for name in ("old", "new", "table", "pages", "count", "lengths", "starts", "slots", "left"):
         assert call(**{name: None}) == -1, name
         assert call(**{name: 0x8002}) == -2, name
+    assert call(capacity=1 << 27) == -2 and call(page=256, capacity=1 << 23) == -2        # more pages than a pool can have
     assert call(lengths=0x2000) == -2                                 # the new lengths are still read while these are written
 
 
