@@ -77,14 +77,15 @@ apbv_status apbv_cache_map(int n_requests, int page_size, int64_t max_blocks,
 /*
  * Writes the rows of k and v ([tokens, n_kv_heads, head_dim] bf16) into the cache, token t at slots[t].  A slot outside
  * [0, n_pages * page_size) (-1: padding) is skipped.  Slots must differ: what a slot named twice holds afterwards is
- * unspecified (other slots are not touched).  tokens == 0 does nothing.
+ * unspecified (other slots are not touched).  tokens == 0 does nothing.  0 <= tokens <= 2^24, and tokens * head_dim / 2048
+ * (rounded up) * n_kv_heads below 2^24; apbv_cache_load alike.
  */
 apbv_status apbv_cache_store(const apbv_cache* cache, int n_kv_heads, int head_dim,
                              apbv_tensor k, apbv_tensor v, const int32_t* slots, void* hip_stream);
 
 /*
  * Reads rows back: k_out, v_out [tokens, n_kv_heads, head_dim] bf16, dense, take the values held at slots[t] (exactly); zero
- * for a slot outside [0, n_pages * page_size).  A slot may be named any number of times.  0 <= tokens <= 2^24.
+ * for a slot outside [0, n_pages * page_size).  A slot may be named any number of times.
  */
 apbv_status apbv_cache_load(const apbv_cache* cache, int n_kv_heads, int head_dim, int64_t tokens,
                             const int32_t* slots, void* k_out, void* v_out, void* hip_stream);
@@ -118,7 +119,7 @@ size_t apbv_cache_attention_workspace_bytes(int n_requests, int64_t n_rows, int 
  * repeatable.
  * Supported: head_dim in {64, 128}; n_q_heads % n_kv_heads == 0; 1 <= n_requests <= 4096; max_blocks * page_size <= 2^30;
  * n_rows * G <= 2^30; (n_rows * G / 16 + n_requests) * n_kv_heads * (max_blocks * page_size / 64) below 2^31 (a table of
- * 4096 rows for 2^20 tokens, with 8 KV heads).
+ * 4096 rows for 2^20 tokens, with 8 KV heads); n_rows * n_q_heads <= 2^26 - 4; n_requests * n_kv_heads below 2^24.
  */
 apbv_status apbv_cache_attention(const apbv_cache* cache, int n_requests, int n_q_heads, int n_kv_heads, int head_dim,
                                  apbv_tensor q, const int32_t* block_table, int64_t table_stride, int64_t max_blocks,

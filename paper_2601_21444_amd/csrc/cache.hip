@@ -133,8 +133,8 @@ __global__ __launch_bounds__(256) void cache_load_kernel(const CacheRowsParams p
 
 template <int D>
 apbv_status launch_rows(const CacheRowsParams& p, bool store, hipStream_t stream) {
-  const int64_t blocks = (p.tokens + RowPiece<D>::kTokens - 1) / RowPiece<D>::kTokens * p.hkv;
-  if (blocks > 0x7fffffff) return APBV_ERR_UNSUPPORTED;
+  static_assert(RowPiece<D>::kTokens == 2048 / D, "cache_row_groups");
+  const int64_t blocks = cache_row_groups(p.tokens, p.hkv, D);
   Launcher launch(stream);
   launch(store ? cache_store_kernel<D> : cache_load_kernel<D>, dim3((unsigned)blocks), dim3(256), 0, p);
   return launch.status();

@@ -565,7 +565,6 @@ void launch_few_rows(Launcher& launch, const CacheAttnParams& p, const CachePlan
 }
 template <int D>
 apbv_status launch_dim(const CacheAttnParams& p, const CachePlan& plan, hipStream_t stream) {
-  if ((int64_t)p.n_rows * p.hq > 0x7fffffff) return APBV_ERR_UNSUPPORTED;
   Launcher launch(stream);
   if (plan.rows == 16) {
     launch_few_rows<D, 1>(launch, p, plan);

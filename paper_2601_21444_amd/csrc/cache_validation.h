@@ -8,6 +8,10 @@ namespace apbv {
 constexpr int64_t kMaxSlots = ((int64_t)1 << 31) - 1;
 constexpr int64_t kMaxCachedTokens = (int64_t)1 << 30;      // of one request
 constexpr int kCacheBlock = 32;             // elements that share a scale
+constexpr int64_t kMaxGroups = (1 << 24) - 1;               // of 256 threads: a launch counts its threads in 32 bits
+
+// Workgroups of a store or load: each takes a head of 2048 / d tokens.
+inline int64_t cache_row_groups(int64_t tokens, int hkv, int d) { return (tokens + 2048 / d - 1) / (2048 / d) * hkv; }
 
 inline bool valid_page_size(int p) { return p == 16 || p == 32 || p == 64 || p == 128 || p == 256; }
 inline int log2_page(int p) { return p == 16 ? 4 : p == 32 ? 5 : p == 64 ? 6 : p == 128 ? 7 : 8; }
@@ -65,7 +69,7 @@ inline apbv_status validate_cache_store(const apbv_cache* cache, int hkv, int d,
   if (k.tokens != v.tokens) return APBV_ERR_SHAPE;
   if (k.tokens > 0 && slots == nullptr) return APBV_ERR_NULL;
   if (!aligned(slots, 4)) return APBV_ERR_SHAPE;
-  return APBV_OK;
+  return cache_row_groups(k.tokens, hkv, d) <= kMaxGroups ? APBV_OK : APBV_ERR_UNSUPPORTED;
 }
 
 inline apbv_status validate_cache_load(const apbv_cache* cache, int hkv, int d, int64_t tokens, const int32_t* slots, const void* k_out,
@@ -75,7 +79,7 @@ inline apbv_status validate_cache_load(const apbv_cache* cache, int hkv, int d, 
   if (tokens < 0 || tokens > kMaxTokens) return APBV_ERR_SHAPE;
   if (tokens > 0 && (slots == nullptr || k_out == nullptr || v_out == nullptr)) return APBV_ERR_NULL;
   if (!aligned(slots, 4) || !aligned(k_out, 16) || !aligned(v_out, 16)) return APBV_ERR_SHAPE;
-  return APBV_OK;
+  return cache_row_groups(tokens, hkv, d) <= kMaxGroups ? APBV_OK : APBV_ERR_UNSUPPORTED;
 }
 
 // The tiles of all (request, KV head, row tile) are numbered in 32 bits; the host knows the most there can be.
@@ -99,6 +103,8 @@ inline apbv_status validate_cache_attention(const apbv_cache* cache, int n_reque
   if (!aligned(lengths, 4) || !aligned(q_starts, 4)) return APBV_ERR_SHAPE;
   if (q_starts == nullptr && q.tokens % n_requests) return APBV_ERR_SHAPE;
   if (q.tokens * (hq / hkv) > (int64_t)1 << 30) return APBV_ERR_UNSUPPORTED;      // rows of a KV head: kept in 32 bits
+  // workgroups of the launches: one for every (request, KV head), or for four (row, head) of the output
+  if ((int64_t)n_requests * hkv > kMaxGroups || q.tokens * hq > 4 * kMaxGroups) return APBV_ERR_UNSUPPORTED;
   if (max_q < 0 || max_q > kMaxTokens) return APBV_ERR_SHAPE;
   if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale)) return APBV_ERR_SHAPE;
   if (q.tokens > 0 && out == nullptr) return APBV_ERR_NULL;

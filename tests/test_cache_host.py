@@ -154,6 +154,17 @@ def test_store_and_load_refuse_bad_arguments_without_launching():
     assert store(k=view(0, 2, 128), v=view(0, 2, 128), slots=None) == 0 and load(n=0, slots=None, k=None, v=None) == 0
 
 
+def test_launches_of_more_threads_than_32_bits_count_are_refused():
+    lib = apbv.load_library()
+    many = 1 << 24
+    c = cache(hkv=16)
+    assert lib.apbv_cache_load(ctypes.byref(c), 16, 128, many, 0x5000, 0x6000, 0x7000, None) == -3
+    assert lib.apbv_cache_store(ctypes.byref(c), 16, 128, view(many, 16, 128), view(many, 16, 128), 0x5000, None) == -3
+    assert call_attention(c=cache(hkv=4), hq=4, hkv=4, q=view(many, 4, 128), starts=0x7000) == -3       # 2^26 rows of the output
+    wide = cache(hkv=4096, page=16, d=64)
+    assert call_attention(c=wide, n=4096, hq=4096, hkv=4096, d=64, q=view(1, 4096, 64), blocks=1, stride=1) == -3
+
+
 def test_map_refuses_bad_arguments_without_launching():
     lib = apbv.load_library()
 
