@@ -114,8 +114,8 @@ size_t apbv_cache_attention_workspace_bytes(int n_requests, int64_t n_rows, int 
  * zeros and -inf.  Keys on a page outside [0, n_pages) are taken as not there.
  *
  * Arithmetic: the cached values are exact in bf16; bf16 operands, fp32 accumulation and softmax, probabilities rounded to
- * bf16 before the product with V and divided by their rounded sum (the lse is of their exact one), the parts of a row that several workgroups share are kept and joined in fp32, output
- * rounded to bf16.  How the keys are cut depends on the shape of the call and on all lengths; results of the same call are
+ * bf16 before the product with V and divided by their rounded sum (the lse is of their exact one), the parts of a row that
+ * several workgroups share are kept and joined in fp32, output rounded to bf16.  How the keys are cut depends on the shape of the call and on all lengths; results of the same call are
  * repeatable.
  * Supported: head_dim in {64, 128}; n_q_heads % n_kv_heads == 0; 1 <= n_requests <= 4096; max_blocks * page_size <= 2^30;
  * n_rows * G <= 2^30; (n_rows * G / 16 + n_requests) * n_kv_heads * (max_blocks * page_size / 64) below 2^31 (a table of

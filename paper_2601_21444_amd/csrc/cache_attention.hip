@@ -300,83 +300,83 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
   // ---- the pieces of a row tile that lie in consecutive waves, one chain of them after the other: chain 0 goes on with a row
   // tile that began before this workgroup, chain c begins with the tail of wave c - 1
   auto put_together = [&]() {
-  if (lane == 0) kept[wave] = keeps;
-  __syncthreads();
-  int heads = 0, tails = 0, spans = 0;                     // a bit a wave
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
-    const int k = __builtin_amdgcn_readfirstlane(kept[w]);
-    heads |= (k & kHead ? 1 : 0) << w;
-    tails |= (k & kTail ? 1 : 0) << w;
-    spans |= (k & kSpan ? 1 : 0) << w;
-  }
-#pragma unroll 1
-  for (int chain = kWhole ? 1 : 0; chain <= (kWhole ? 1 : W); ++chain) {
-    const int from = chain == 0 ? 0 : chain - 1;
-    if (((chain == 0 ? heads | spans : tails) >> from & 1) == 0) continue;
-    int to = from;                                         // its last wave
-    bool ends = chain == 0 && (heads & 1);
-    while (!ends && to + 1 < W) {
-      if (heads >> (to + 1) & 1) ends = true;
-      else if ((spans >> (to + 1) & 1) == 0) break;        // a wave without a share: the workgroup ends here
-      ++to;
+    if (lane == 0) kept[wave] = keeps;
+    __syncthreads();
+    int heads = 0, tails = 0, spans = 0;                     // a bit a wave
+  #pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const int k = __builtin_amdgcn_readfirstlane(kept[w]);
+      heads |= (k & kHead ? 1 : 0) << w;
+      tails |= (k & kTail ? 1 : 0) << w;
+      spans |= (k & kSpan ? 1 : 0) << w;
     }
-    const bool whole = kWhole || (chain > 0 && ends);
-    const int* at = place[ends && to == from ? 1 : 0][from];
-    const int first = at[0], rows = at[1], head = at[2], r0 = at[3];
-    const int slot = chain > 0 ? 1 : 0;                    // a part that begins a row tile, or one that goes on with it
-    float* part = p.parts + ((int64_t)wg * 2 + slot) * (R * D);
-    float* part_stat = part_stats(p, slot, R, D) + wg;
-    for (int x = threadIdx.x; x < R * (D / 8); x += 64 * W) {
-      const int row = x / (D / 8), c = x % (D / 8);
-      if (r0 + row >= rows) break;
-      // (all waves' statistics, then all waves' rows, are read at once, those of others than the chain's left out)
-      float m_of[W], l = 0.f, exact = 0.f, m = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        m_of[w] = stat[w == to && ends ? 1 : 0][w][0][row];
-        m_of[w] = w >= from && w <= to ? m_of[w] : -INFINITY;
-        m = fmaxf(m, m_of[w]);
+  #pragma unroll 1
+    for (int chain = kWhole ? 1 : 0; chain <= (kWhole ? 1 : W); ++chain) {
+      const int from = chain == 0 ? 0 : chain - 1;
+      if (((chain == 0 ? heads | spans : tails) >> from & 1) == 0) continue;
+      int to = from;                                         // its last wave
+      bool ends = chain == 0 && (heads & 1);
+      while (!ends && to + 1 < W) {
+        if (heads >> (to + 1) & 1) ends = true;
+        else if ((spans >> (to + 1) & 1) == 0) break;        // a wave without a share: the workgroup ends here
+        ++to;
       }
-      const float m0 = m > -INFINITY ? m : 0.f;
-      f32x4 x0 = {0.f, 0.f, 0.f, 0.f}, x1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        if (w < from || w > to) continue;
-        const int is_head = w == to && ends ? 1 : 0;
-        const float weight = __builtin_amdgcn_exp2f(m_of[w] - m0);
-        l = __builtin_fmaf(stat[is_head][w][1][row], weight, l);
-        if (kLse) exact = __builtin_fmaf(stat[is_head][w][2][row], weight, exact);
-        with_kept(is_head, w, [&](const f32x4* src) {
-          src += row * kChunks;
-          x0 += weight * src[(2 * c) ^ (row & 15)];
-          x1 += weight * src[(2 * c + 1) ^ (row & 15)];
-        });
-      }
-      if (whole) {
-        const float inv = l > 0.f ? 1.0f / l : 0.f;
-        x0 *= inv;
-        x1 *= inv;
-        u32x4 y;
-        y.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x0.x, x0.y}), bf16x2));
-        y.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x0.z, x0.w}), bf16x2));
-        y.z = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x1.x, x1.y}), bf16x2));
-        y.w = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x1.z, x1.w}), bf16x2));
-        const int i = query_of(p, r0 + row), h = head * p.group + r0 + row - i * p.group;
-        *reinterpret_cast<u32x4*>(p.out + ((int64_t)(first + i) * p.hq + h) * D + 8 * c) = y;
-        if (kLse && c == 0) p.lse[(int64_t)h * p.n_rows + first + i] = log_sum(m, exact);
-      } else {
-        f32x4* dst = reinterpret_cast<f32x4*>(part + row * D + 8 * c);
-        dst[0] = x0;
-        dst[1] = x1;
-        if (c == 0) {
-          part_stat[(int64_t)row * p.workgroups] = m;
-          part_stat[(int64_t)(R + row) * p.workgroups] = l;
-          if (kLse) part_stat[(int64_t)(2 * R + row) * p.workgroups] = exact;
+      const bool whole = kWhole || (chain > 0 && ends);
+      const int* at = place[ends && to == from ? 1 : 0][from];
+      const int first = at[0], rows = at[1], head = at[2], r0 = at[3];
+      const int slot = chain > 0 ? 1 : 0;                    // a part that begins a row tile, or one that goes on with it
+      float* part = p.parts + ((int64_t)wg * 2 + slot) * (R * D);
+      float* part_stat = part_stats(p, slot, R, D) + wg;
+      for (int x = threadIdx.x; x < R * (D / 8); x += 64 * W) {
+        const int row = x / (D / 8), c = x % (D / 8);
+        if (r0 + row >= rows) break;
+        // (all waves' statistics, then all waves' rows, are read at once, those of others than the chain's left out)
+        float m_of[W], l = 0.f, exact = 0.f, m = -INFINITY;
+  #pragma unroll
+        for (int w = 0; w < W; ++w) {
+          m_of[w] = stat[w == to && ends ? 1 : 0][w][0][row];
+          m_of[w] = w >= from && w <= to ? m_of[w] : -INFINITY;
+          m = fmaxf(m, m_of[w]);
+        }
+        const float m0 = m > -INFINITY ? m : 0.f;
+        f32x4 x0 = {0.f, 0.f, 0.f, 0.f}, x1 = {0.f, 0.f, 0.f, 0.f};
+  #pragma unroll
+        for (int w = 0; w < W; ++w) {
+          if (w < from || w > to) continue;
+          const int is_head = w == to && ends ? 1 : 0;
+          const float weight = __builtin_amdgcn_exp2f(m_of[w] - m0);
+          l = __builtin_fmaf(stat[is_head][w][1][row], weight, l);
+          if (kLse) exact = __builtin_fmaf(stat[is_head][w][2][row], weight, exact);
+          with_kept(is_head, w, [&](const f32x4* src) {
+            src += row * kChunks;
+            x0 += weight * src[(2 * c) ^ (row & 15)];
+            x1 += weight * src[(2 * c + 1) ^ (row & 15)];
+          });
+        }
+        if (whole) {
+          const float inv = l > 0.f ? 1.0f / l : 0.f;
+          x0 *= inv;
+          x1 *= inv;
+          u32x4 y;
+          y.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x0.x, x0.y}), bf16x2));
+          y.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x0.z, x0.w}), bf16x2));
+          y.z = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x1.x, x1.y}), bf16x2));
+          y.w = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x1.z, x1.w}), bf16x2));
+          const int i = query_of(p, r0 + row), h = head * p.group + r0 + row - i * p.group;
+          *reinterpret_cast<u32x4*>(p.out + ((int64_t)(first + i) * p.hq + h) * D + 8 * c) = y;
+          if (kLse && c == 0) p.lse[(int64_t)h * p.n_rows + first + i] = log_sum(m, exact);
+        } else {
+          f32x4* dst = reinterpret_cast<f32x4*>(part + row * D + 8 * c);
+          dst[0] = x0;
+          dst[1] = x1;
+          if (c == 0) {
+            part_stat[(int64_t)row * p.workgroups] = m;
+            part_stat[(int64_t)(R + row) * p.workgroups] = l;
+            if (kLse) part_stat[(int64_t)(2 * R + row) * p.workgroups] = exact;
+          }
         }
       }
     }
-  }
   };
 
   if constexpr (kWhole) {
