@@ -61,7 +61,7 @@ typedef struct {
  *                             count outside [0, free_capacity] counts as the nearest in it; pages beyond the capacity are lost
  *   lengths_out               [n_requests] int32; may be old_lengths, not new_lengths
  *   starts_out                [n_requests + 1] int32;  slots_out [max_new_tokens] int32 (may be NULL if that is 0)
- *   free_count_out            [1] int32; may be free_count
+ *   free_count_out            [1] int32; may be free_count (in place: a second launch where max_new_tokens exceeds 8192)
  * 1 <= n_requests <= 4096; 0 <= max_new_tokens <= 2^24; 1 <= max_blocks, max_blocks * page_size <= 2^30;
  * 0 <= free_capacity, free_capacity * page_size < 2^31 (no pool has more pages).
  */

@@ -7,11 +7,11 @@
 // Both directions move bytes and are bound by them: 16384 tokens of 4 heads of 128 are written in 9.6 us (4.4 TB/s) and read
 // back in 6.6 (6.4 TB/s); from 64 tokens a launch's 2.5 us are all.
 //
-// Tables.  The lengths are few thousand integers: one workgroup takes their prefix sums and does what depends on the order of
-// the requests (pages given back, pages taken).  The slots of a step's few tokens are found by the same workgroup; those of
-// prompts, of which there may be a hundred thousand, by a second launch over the tokens.  Bound by the chain of launch, lengths,
-// prefix sums and pages: 64 requests of one token 3.9 us, of which a launch that only reads and writes takes 2.5; 48 prompts of
-// 80000 tokens 12.0 with the second launch (4.1).
+// Tables.  The lengths are few thousand integers: a workgroup takes their prefix sums, finds which requests are granted, and then
+// deals tokens and pages to its threads.  A hundred thousand tokens of prompts are dealt to as many workgroups as they fill, each
+// of which takes the sums for itself; in place, where one would write what another has yet to read, one workgroup does all but
+// the slots, which a second launch finds.  Bound by the chain of launch, lengths, prefix sums and pages: 64 requests of one token
+// 3.9 us, of which a launch that only reads and writes takes 2.5; 48 prompts of 80000 tokens 6.6, in place 12.0.
 #include "cache.h"
 
 namespace apbv {
@@ -143,7 +143,7 @@ apbv_status launch_rows(const CacheRowsParams& p, bool store, hipStream_t stream
 // ---- tables
 
 constexpr int kMapThreads = 1024;
-constexpr int kMapSlots = 8192;             // new tokens up to which the one workgroup finds the slots too
+constexpr int kMapSlots = 8192;             // new tokens up to which one workgroup finds the slots too, in place
 constexpr int kTop = 0x7fffffff;
 
 __device__ __forceinline__ int clamp_int(int64_t x, int lo, int hi) { return (int)(x < lo ? lo : (x > hi ? hi : x)); }
@@ -177,7 +177,9 @@ __device__ __forceinline__ int slot_of(int page, int pos, int page_log2) {
   return (page << page_log2) + (pos & ((1 << page_log2) - 1));
 }
 
-// One workgroup.  A thread holds kPer consecutive requests in registers and knows, after the prefix sums, where their tokens and
+// One workgroup, or several where nothing that they write is read by another: where the outputs are not the inputs.  All find
+// the same sums; the first writes what there is one of a request, tokens and pages are dealt to the threads of all.
+// A thread holds kPer consecutive requests in registers and knows, after the prefix sums, where their tokens and
 // pages lie.  In a decoding step, where no request grows by more than kFew tokens, that is all it takes: every thread serves
 // its own requests.  Otherwise, and for pages given back, tokens and pages are dealt to the threads, which find the request of
 // each in LDS.  Pages are taken from where the list has them or will have them, so that nothing written here is read here: two
@@ -193,6 +195,7 @@ __global__ __launch_bounds__(kMapThreads) void cache_map_kernel(const CacheMapPa
   __shared__ int wave_sum[kWaves][4];          // the three sums, and whether a request grows by many tokens
   __shared__ int n_taken;
   const int n = p.n_requests, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b0 = threadIdx.x * kPer;
+  const int of_all = blockIdx.x * kMapThreads + threadIdx.x, all = gridDim.x * kMapThreads;
   auto blocks = [&](int length) { return (int)(((uint32_t)length + (1u << p.page_log2) - 1) >> p.page_log2); };
   auto table_at = [&](int b, int block) -> int32_t* { return p.table + (int64_t)b * p.table_stride + block; };
 
@@ -265,12 +268,12 @@ __global__ __launch_bounds__(kMapThreads) void cache_map_kernel(const CacheMapPa
     before[2] = add_stop(before[2], up < 0 ? -up : 0);
     granted[u] = possible[u] && (grown[u] == 0 || (before[0] <= p.max_new && (up == 0 || before[1] <= free)));
     if (granted[u] && up > 0) last_taken = before[1];
-    if (b < n) {
+    if (b < n && blockIdx.x == 0) {
       p.lengths_out[b] = granted[u] ? want[u] : had[u];
       p.starts_out[b] = first[0][u] < p.max_new ? first[0][u] : p.max_new;
     }
   }
-  if (threadIdx.x == 0) p.starts_out[n] = total[0] < p.max_new ? total[0] : p.max_new;
+  if (of_all == 0) p.starts_out[n] = total[0] < p.max_new ? total[0] : p.max_new;
   if (last_taken > 0) atomicMax(&n_taken, last_taken);
   if (!own || n_back > 0) {
 #pragma unroll
@@ -285,7 +288,7 @@ __global__ __launch_bounds__(kMapThreads) void cache_map_kernel(const CacheMapPa
     if (threadIdx.x == 0) first_token[n] = total[0], first_taken[n] = total[1], first_back[n] = total[2];
   }
   __syncthreads();
-  if (threadIdx.x == 0) *p.free_count_out = free - n_taken;
+  if (of_all == 0) *p.free_count_out = free - n_taken;
 
   // a page given back, the i-th: one of the last blocks its request had; entry i of the list as it stands then
   auto back = [&](int i) -> const int32_t* {
@@ -298,7 +301,7 @@ __global__ __launch_bounds__(kMapThreads) void cache_map_kernel(const CacheMapPa
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
       const int b = b0 + u, old = blocks(had[u]), up = blocks(want[u]) - old;
-      if (b >= n || grown[u] == 0) continue;
+      if (b >= n || grown[u] == 0 || blockIdx.x != 0) continue;
       int page_old = -1, page_new = -1;
       if (granted[u]) {
         if ((had[u] & ((1 << p.page_log2) - 1)) != 0) page_old = *table_at(b, old - 1);
@@ -313,15 +316,15 @@ __global__ __launch_bounds__(kMapThreads) void cache_map_kernel(const CacheMapPa
         }
     }
     if (with_slots)
-      for (int t = total[0] + threadIdx.x; t >= 0 && t < p.max_new; t += kMapThreads) p.slots_out[t] = -1;
+      for (int64_t t = (int64_t)total[0] + of_all; t < p.max_new; t += all) p.slots_out[t] = -1;
   } else {
     const int taken = n_taken;
-    for (int i = threadIdx.x; i < taken; i += kMapThreads) {
+    for (int i = of_all; i < taken; i += all) {
       const int b = owner(first_taken, n, i);
       *table_at(b, blocks((int)(had_granted[b] & kTop)) + (i - first_taken[b])) = *entry(free - 1 - i);
     }
     if (with_slots)
-      for (int t = threadIdx.x; t < p.max_new; t += kMapThreads) {
+      for (int t = of_all; t < p.max_new; t += all) {
         int slot = -1;
         if (t < total[0]) {
           const int b = owner(first_token, n, t);
@@ -333,7 +336,7 @@ __global__ __launch_bounds__(kMapThreads) void cache_map_kernel(const CacheMapPa
         p.slots_out[t] = slot;
       }
   }
-  for (int i = threadIdx.x; i < n_back && i < p.free_capacity - held; i += kMapThreads) p.free_pages[held + i] = *back(i);
+  for (int i = of_all; i < n_back && i < p.free_capacity - held; i += all) p.free_pages[held + i] = *back(i);
 }
 
 // The slots of many new tokens, from what the first launch wrote: a request that was refused kept another length than it
@@ -377,9 +380,12 @@ apbv_status launch_cache_load(const CacheRowsParams& p, int head_dim, hipStream_
 
 apbv_status launch_cache_map(const CacheMapParams& p, hipStream_t stream) {
   Launcher launch(stream);
-  const int with_slots = p.max_new <= kMapSlots;
+  // in place, one workgroup and, for many tokens, a second launch; otherwise a workgroup for 1024 tokens, two a compute unit at most
+  const bool in_place = p.lengths_out == p.old_lengths || p.free_count_out == p.free_count;
+  const int with_slots = !in_place || p.max_new <= kMapSlots;
+  const int groups = in_place ? 1 : p.max_new <= kMapThreads ? 1 : p.max_new < 512 * kMapThreads ? (p.max_new + kMapThreads - 1) / kMapThreads : 512;
   static_assert(4 * kMapThreads == APBV_CACHE_MAX_REQUESTS, "a thread's requests");
-  launch(p.n_requests <= kMapThreads ? cache_map_kernel<1> : cache_map_kernel<4>, dim3(1), dim3(kMapThreads), 0, p, with_slots);
+  launch(p.n_requests <= kMapThreads ? cache_map_kernel<1> : cache_map_kernel<4>, dim3(groups), dim3(kMapThreads), 0, p, with_slots);
   if (!with_slots) {
     const unsigned per = 256 * kSlotsPerThread;
     launch(cache_slots_kernel, dim3(((unsigned)p.max_new + per - 1) / per), dim3(256), 0, p);

@@ -171,6 +171,24 @@ def test_map_matches_the_oracle(n, page, blocks, tight):
         assert args[0].tolist() == old and args[1].tolist() == new and args[4].tolist() == [count]
 
 
+@pytest.mark.parametrize("alias", ["lengths", "count", "both"])
+@pytest.mark.parametrize("n,page,blocks", [(3, 32, 7), (64, 64, 40), (300, 128, 5), (4096, 16, 3), (7, 256, 200)])
+def test_map_in_place_matches_the_oracle(n, page, blocks, alias):
+    rng = np.random.default_rng((3, n, page, blocks))
+    for tight in (False, True):
+        old, new, table, free, count, most = random_step(rng, n, page, blocks, tight)
+        print("map in place", n, page, blocks, tight, "new tokens", most, flush=True)
+        args = dev_int(old), dev_int(new), dev_int(table), dev_int(free), dev_int([count])
+        kw = {}
+        if alias != "count":
+            kw["lengths_out"] = args[0]
+        if alias != "lengths":
+            kw["free_count_out"] = args[4]
+        got = [x.tolist() for x in apbv.apbv_cache_map(*args, page, most, **kw)]
+        want = co.cache_map(old, new, table, free, count, page, most)
+        assert got == list(want[:3]) + [[want[3]]] and args[2].tolist() == table and args[3].tolist() == free
+
+
 def test_map_in_place_and_a_list_that_is_full():
     """lengths_out is old_lengths, free_count_out free_count; what is given back beyond the list's capacity is dropped."""
     old, new, table, free, count = [40, 0, 100], [0, 33, 101], [[1, 2, 3, 0, 0, 0, 0], [0] * 7, [4, 5, 6, 7, 8, 9, 10]], [30, 31], 1
