@@ -57,7 +57,7 @@ struct CacheAttnParams {
   int n_requests, n_rows, each;     // each: rows of every request where starts is nullptr
   int max_len;             // the longest length a row of the table holds
   int hq, hkv, group, causal;
-  int workgroups, short_tiles, least_tiles;
+  int workgroups, short_tiles, least_tiles, share_step;
   int row_tiles;           // of a request, by max_q
   float scale_log2;        // softmax_scale * log2(e)
   double per_group;        // 1 / group

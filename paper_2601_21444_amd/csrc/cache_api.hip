@@ -94,6 +94,7 @@ apbv_status apbv_cache_attention(const apbv_cache* cache, int n_requests, int n_
   p.workgroups = plan.workgroups;
   p.short_tiles = plan.short_tiles;
   p.least_tiles = plan.least_tiles;
+  p.share_step = plan.share_step;
   p.row_tiles = plan.row_tiles;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
   p.per_group = 1.0 / p.group;

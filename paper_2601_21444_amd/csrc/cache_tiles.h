@@ -129,7 +129,9 @@ struct Axis {
   __device__ __forceinline__ uint32_t share(const CacheAttnParams& p) const {
     uint32_t q = (total + (uint32_t)p.workgroups - 1) / (uint32_t)p.workgroups;
     if (q < (uint32_t)p.short_tiles) q = (total + (uint32_t)p.workgroups / 2 - 1) / ((uint32_t)p.workgroups / 2);
-    return q > (uint32_t)p.least_tiles ? q : (uint32_t)p.least_tiles;
+    q = q > (uint32_t)p.least_tiles ? q : (uint32_t)p.least_tiles;
+    if (q > 3 * (uint32_t)p.share_step) q = (q + (uint32_t)p.share_step - 1) / (uint32_t)p.share_step * (uint32_t)p.share_step;
+    return q;
   }
   // The share of this workgroup, or -1: consecutive shares on one XCD (row tiles of a head read the same keys), which a launch
   // gives its workgroups in turn.

@@ -122,6 +122,7 @@ struct CachePlan {
   int workgroups;
   int short_tiles;   // where shares would be shorter than this, half as many workgroups share the axis
   int least_tiles;   // a share is not shorter than this
+  int share_step;    // a share of more than three times this is a multiple of it
   int row_tiles;     // of a request
   bool whole;        // a workgroup for every (request, KV head, row tile)
   int join_waves;    // waves that join the parts of a row: 1 or 4
@@ -131,6 +132,13 @@ struct CachePlan {
 // 512, 20.3 / 19.3; 256 requests of 65 to 2048 keys, 8 / 2 heads of 64, 9 tiles, 21.6 / 22.9; 64 queries over 16512 keys, 4 tiles,
 // 36 / 34; 64 requests of 512 to 32768 keys, 28 / 4 heads of 128, 56 tiles, 50.6 / 52.0).  Shares of one tile rather than two cost
 // the join more than they save (16000 keys 12.4 / 11.8; 64 queries over 2000 keys 21.6 / 17.4).
+//
+// Few row tiles of 16 rows have hardly an end inside a workgroup, which a second one would fill with work: one is enough at
+// head_dim 128, however long (one query, 16 / 2 heads, 512 / 256 workgroups: 262144 keys 26.5 / 23.3, 524288 37.0 / 33.2; 64 / 8
+// heads, 400000 keys 89.5 / 86.9; with pages of 16 tokens 262144 keys 28.4 / 26.5, 500000 37.6 / 39.0), and below 12 tiles each at
+// 64 (8 / 2 heads: 133120 keys, 8 tiles each of 512, 15.1 / 13.4; 500000, 31 tiles, 23.9 / 24.6).  Their waves take equally many
+// tiles where that makes a share not much longer: the longest part is as long as before, and there are fewer to join (133120
+// keys, 17 or 20 tiles a share: 18.7 / 18.1; of 5 or 8, 40000 keys: 13.0 / 14.1; 64 requests, 57 or 60: 51.7 / 52.5).
 //
 // Where the table holds but a few tiles a request, a workgroup takes a whole (request, KV head, row tile): no axis to plan, no
 // parts, no second launch.  It is alone with its keys, so a table of longer requests, or one of 2048 tokens where there are few,
@@ -147,9 +155,11 @@ inline CachePlan choose_cache_plan(int n_requests, int hq, int hkv, int d, int64
   CachePlan p;
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kCacheBlockRows;
   p.workgroups = 512;
-  p.short_tiles = d == 128 ? 12 : 6;
-  p.least_tiles = 2;
   p.row_tiles = rows <= p.rows ? 1 : (int)((rows + p.rows - 1) / p.rows);
+  const bool few = p.rows == 16 && (int64_t)n_requests * hkv <= 8;
+  p.short_tiles = few && d == 128 ? 1 << 30 : few || d == 128 ? 12 : 6;
+  p.least_tiles = 2;
+  p.share_step = few ? kCacheWaves : 1;
   const int64_t longest = (max_len + kCacheKeyTile - 1) / kCacheKeyTile;
   p.whole = p.rows != kCacheBlockRows && (longest <= 20 || (longest <= 32 && (int64_t)n_requests * hkv * p.row_tiles >= 64));
   const int64_t parts = p.workgroups / ((int64_t)n_requests * hkv * p.row_tiles) + 1;      // of a row, if the requests are alike
