@@ -106,7 +106,16 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     constexpr int kAhead = NQ == 1 ? 2 : 1;
     Codes<D> kc[kAhead][4], vc[kAhead][4];
     Blocks<D, kOnePage> at[kAhead];
-    auto find = [&](auto& x, int t) { x.find(p, table_row, head, rq.len, t < t_end ? t : t_end - 1); };      // (the last tile again)
+    auto tile = [&](int t) { return t < t_end ? t : t_end - 1; };          // (the last tile again)
+    int next_page = 0;                                     // of smaller pages: looked up for the next tile to find
+    auto find = [&](auto& x, int t) {
+      if constexpr (kOnePage) {
+        x.find(p, table_row, head, rq.len, tile(t));
+      } else {
+        x.place(p, head, rq.len, tile(t), next_page);
+        next_page = x.look_up(p, table_row, rq.len, tile(t + 1));
+      }
+    };
     auto load_k = [&](const auto& x, Codes<D> (&to)[4]) { x.load(to, p.cache.k_codes, p.cache.k_scales, li, lg); };
     auto load_v = [&](const auto& x, Codes<D> (&to)[4]) { x.load(to, p.cache.v_codes, p.cache.v_scales, li, lg); };
     auto work = [&](int t, Blocks<D, kOnePage>& here, Codes<D> (&kc)[4], Codes<D> (&vc)[4]) {
@@ -216,6 +225,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     };
     int t = t0;
     if (t < t_end) {
+      if constexpr (!kOnePage) next_page = at[0].look_up(p, table_row, rq.len, t);
 #pragma unroll
       for (int a = 0; a < kAhead; ++a) find(at[a], t + a);
 #pragma unroll

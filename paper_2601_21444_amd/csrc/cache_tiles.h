@@ -188,36 +188,58 @@ struct Codes {
   }
 };
 
-// Where the four 16-key blocks of a tile lie (uniform), as byte offsets into the codes and the scales of K and of V, and which
-// blocks are not there.  A page of 64 tokens or more holds a whole tile: one lookup, and the blocks follow one another.
+// Where the four 16-key blocks of a tile lie, as byte offsets into the codes and the scales of K and of V, and which blocks are
+// not there.  A page of 64 tokens or more holds a whole tile: one lookup, uniform, and the blocks follow one another.
 template <int D, bool kOnePage>
 struct Blocks {
-  static constexpr int kLookups = kOnePage ? 1 : 4;
-  int64_t codes[kLookups], scales[kLookups];
-  int absent;                // bit i: the page of lookup i is out of range, or no key of the request lies in it
+  int64_t codes, scales;
+  int absent;                // the page is out of range, or no key of the request lies in it
   __device__ __forceinline__ void find(const CacheAttnParams& p, const int32_t* table_row, int head, int len, int tile) {
-    absent = 0;
-#pragma unroll
-    for (int i = 0; i < kLookups; ++i) {
-      const int token = tile * kCacheKeyTile + 16 * i;
-      const int at = token < len ? token : len - 1;                      // (a table entry that the request has)
-      const int page = scalar_load(table_row, at >> p.cache.page_log2);
-      const bool there = token < len && (unsigned)page < (unsigned)p.cache.n_pages;
-      absent |= there ? 0 : 1 << i;
-      const int pg = there ? page : 0;
-      const int row = (head << p.cache.page_log2) + (token & ((1 << p.cache.page_log2) - 1));
-      codes[i] = (int64_t)((uint64_t)(uint32_t)pg * (uint32_t)p.cache.stride_codes) + (uint32_t)row * (uint32_t)(D / 2);
-      scales[i] = (int64_t)((uint64_t)(uint32_t)pg * (uint32_t)p.cache.stride_scales) + (uint32_t)row * (uint32_t)(D / 32);
-    }
+    const int token = tile * kCacheKeyTile, at = token < len ? token : len - 1;      // (a table entry that the request has)
+    const int page = scalar_load(table_row, at >> p.cache.page_log2);
+    const bool there = token < len && (unsigned)page < (unsigned)p.cache.n_pages;
+    absent = there ? 0 : 1;
+    const int pg = there ? page : 0;
+    const int row = (head << p.cache.page_log2) + (token & ((1 << p.cache.page_log2) - 1));
+    codes = (int64_t)((uint64_t)(uint32_t)pg * (uint32_t)p.cache.stride_codes) + (uint32_t)row * (uint32_t)(D / 2);
+    scales = (int64_t)((uint64_t)(uint32_t)pg * (uint32_t)p.cache.stride_scales) + (uint32_t)row * (uint32_t)(D / 32);
   }
-  __device__ __forceinline__ bool gone(int kb) const { return (absent >> (kOnePage ? 0 : kb) & 1) != 0; }
+  __device__ __forceinline__ bool gone(int) const { return absent != 0; }
   // this lane's pieces of the four blocks of K or of V
   __device__ __forceinline__ void load(Codes<D> (&x)[4], const uint8_t* code_base, const uint8_t* scale_base, int li, int lg) const {
 #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-      constexpr int kCodeStep = kOnePage ? 16 * (D / 2) : 0, kScaleStep = kOnePage ? 16 * (D / 32) : 0;
-      x[kb].load(code_base + codes[kOnePage ? 0 : kb], scale_base + scales[kOnePage ? 0 : kb], kb * kCodeStep, kb * kScaleStep, li, lg);
-    }
+    for (int kb = 0; kb < 4; ++kb) x[kb].load(code_base + codes, scale_base + scales, kb * 16 * (D / 2), kb * 16 * (D / 32), li, lg);
+  }
+};
+// Smaller pages: lane n of every four has the n-th block's place, and looks its page up a tile before it is needed (us, four times
+// in scalar instructions / so: one query over 700 keys, 2 / 1 heads of 64, pages of 16 7.5 / 6.7; 256 requests of 65 to 2048 keys,
+// 8 / 2 heads of 64, pages of 32 15.4 / 14.7).
+template <int D>
+struct Blocks<D, false> {
+  int64_t codes, scales;
+  int absent;                // bit i: of block i, uniform
+  __device__ __forceinline__ static int token_of(int tile) { return tile * kCacheKeyTile + 16 * (int)(threadIdx.x & 3); }
+  __device__ __forceinline__ static int look_up(const CacheAttnParams& p, const int32_t* table_row, int len, int tile) {
+    const int token = token_of(tile);
+    return table_row[(token < len ? token : len - 1) >> p.cache.page_log2];
+  }
+  __device__ __forceinline__ void place(const CacheAttnParams& p, int head, int len, int tile, int page) {
+    const int token = token_of(tile);
+    const bool there = token < len && (unsigned)page < (unsigned)p.cache.n_pages;
+    absent = (int)(~__builtin_amdgcn_ballot_w64(there) & 15);
+    const int pg = there ? page : 0;
+    const int row = (head << p.cache.page_log2) + (token & ((1 << p.cache.page_log2) - 1));
+    codes = (int64_t)((uint64_t)(uint32_t)pg * (uint32_t)p.cache.stride_codes) + (uint32_t)row * (uint32_t)(D / 2);
+    scales = (int64_t)((uint64_t)(uint32_t)pg * (uint32_t)p.cache.stride_scales) + (uint32_t)row * (uint32_t)(D / 32);
+  }
+  __device__ __forceinline__ bool gone(int kb) const { return (absent >> kb & 1) != 0; }
+  __device__ __forceinline__ static int64_t of_block(int64_t x, int kb) {
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, kb), hi = __builtin_amdgcn_readlane((uint32_t)((uint64_t)x >> 32), kb);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+  }
+  __device__ __forceinline__ void load(Codes<D> (&x)[4], const uint8_t* code_base, const uint8_t* scale_base, int li, int lg) const {
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) x[kb].load(code_base + of_block(codes, kb), scale_base + of_block(scales, kb), 0, 0, li, lg);
   }
 };
 
