@@ -101,26 +101,33 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
     }
 
     const int32_t* table_row = p.table + (int64_t)b * p.table_stride;
-    // With one block of rows two tiles are on their way while one is worked on: in a long request a wave has only a few, and
-    // what takes time is how often it waits for memory.  (With two there are no registers for it.)
-    constexpr int kAhead = NQ == 1 ? 2 : 1;
-    Codes<D> kc[kAhead][4], vc[kAhead][4];
-    Blocks<D, kOnePage> at[kAhead];
+    // One tile is on its way while one is worked on.  (Two, us, with / without: one query over 133120 keys, 16 / 2 heads of 128 18.5 /
+    // 17.9; 64 requests of 512 to 32768, 28 / 4 heads 51.0 / 48.9; 256 of 65 to 1200 24.2 / 21.5; 256 of 65 to 2048, 8 / 2 heads of 64,
+    // pages of 32 14.7 / 13.6; 64 of 2048, pages of 64 10.9 / 10.9.)
+    Codes<D> kc[4], vc[4];
+    Blocks<D, kOnePage> here;
     auto tile = [&](int t) { return t < t_end ? t : t_end - 1; };          // (the last tile again)
     int next_page = 0;                                     // of smaller pages: looked up for the next tile to find
-    auto find = [&](auto& x, int t) {
+    auto find = [&](int t) {
       if constexpr (kOnePage) {
-        x.find(p, table_row, head, rq.len, tile(t));
+        here.find(p, table_row, head, rq.len, tile(t));
       } else {
-        x.place(p, head, rq.len, tile(t), next_page);
-        next_page = x.look_up(p, table_row, rq.len, tile(t + 1));
+        here.place(p, head, rq.len, tile(t), next_page);
+        next_page = here.look_up(p, table_row, rq.len, tile(t + 1));
       }
     };
-    auto load_k = [&](const auto& x, Codes<D> (&to)[4]) { x.load(to, p.cache.k_codes, p.cache.k_scales, li, lg); };
-    auto load_v = [&](const auto& x, Codes<D> (&to)[4]) { x.load(to, p.cache.v_codes, p.cache.v_scales, li, lg); };
-    auto work = [&](int t, Blocks<D, kOnePage>& here, Codes<D> (&kc)[4], Codes<D> (&vc)[4]) {
+    auto load_k = [&]() { here.load(kc, p.cache.k_codes, p.cache.k_scales, li, lg); };
+    auto load_v = [&]() { here.load(vc, p.cache.v_codes, p.cache.v_scales, li, lg); };
+    if (t0 < t_end) {
+      if constexpr (!kOnePage) next_page = here.look_up(p, table_row, rq.len, t0);
+      find(t0);
+      load_k();
+      load_v();
+    }
+#pragma unroll 1
+    for (int t = t0; t < t_end; ++t) {
       const Blocks<D, kOnePage> now = here;
-      find(here, t + kAhead);
+      find(t + 1);
 
       // ---- S^T = K Q^T, lane: keys 16 kb + 4 lg + e of row li
       f32x4 s[4][NQ];
@@ -133,7 +140,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
           for (int nq = 0; nq < NQ; ++nq)
             s[kb][nq] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[c][nq], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[kb][nq], 0, 0, 0);
         }
-      load_k(here, kc);
+      load_k();
 
       // ---- hidden keys: out of sight of a row, or not there at all, whose values may be anything
       if ((t + 1) * kCacheKeyTile > all || now.absent != 0) {
@@ -221,27 +228,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
             o[d][nq] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, pw[nq]), o[d][nq], 0, 0, 0);
         }
       }
-      load_v(here, vc);
-    };
-    int t = t0;
-    if (t < t_end) {
-      if constexpr (!kOnePage) next_page = at[0].look_up(p, table_row, rq.len, t);
-#pragma unroll
-      for (int a = 0; a < kAhead; ++a) find(at[a], t + a);
-#pragma unroll
-      for (int a = 0; a < kAhead; ++a) {
-        load_k(at[a], kc[a]);
-        load_v(at[a], vc[a]);
-      }
-#pragma unroll 1
-      for (;;) {
-        work(t, at[0], kc[0], vc[0]);
-        if (++t >= t_end) break;
-        if constexpr (kAhead > 1) {
-          work(t, at[1], kc[1], vc[1]);
-          if (++t >= t_end) break;
-        }
-      }
+      load_v();
     }
 
     // ---- a piece that is a whole row tile is done; others are kept for the waves' pieces to be put together below
