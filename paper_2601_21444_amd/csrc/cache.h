@@ -54,6 +54,7 @@ struct CacheAttnParams {
   // [workgroups][2][rows][d]: O, not divided by the row sum; then [2][3][rows][workgroups]: maxima, sums of the weights as rounded
   // for the product with V, and, where the log-sum-exp is wanted, as they were before; then room for pieces (cache_attention.hip)
   float* parts;
+  uint32_t* begins;        // [1 + n_requests], behind them: the length of a share, and where each request begins on the axis (more than 64)
   int n_requests, n_rows, each;     // each: rows of every request where starts is nullptr
   int max_len;             // the longest length a row of the table holds
   int hq, hkv, group, causal;

@@ -83,6 +83,7 @@ apbv_status apbv_cache_attention(const apbv_cache* cache, int n_requests, int n_
   p.out = static_cast<bf16_t*>(out);
   p.lse = lse_out;
   p.parts = static_cast<float*>(workspace);
+  p.begins = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + cache_parts_bytes(plan, head_dim));
   p.n_requests = n_requests;
   p.n_rows = (int)q.tokens;
   p.each = (int)(q.tokens / n_requests);

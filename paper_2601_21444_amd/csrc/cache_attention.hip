@@ -426,6 +426,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
       const uint32_t rel = pos - begin, item = rel / (uint32_t)rq.tiles;
       const int head = (int)(item / (uint32_t)row_tiles), rt = (int)(item - (uint32_t)head * row_tiles);
       const int t0 = (int)(rel - item * (uint32_t)rq.tiles);
+      if (rel == 0) axis.leave_word(p, b, begin, share);
       const int t1 = end - pos < (uint32_t)(rq.tiles - t0) ? t0 + (int)(end - pos) : rq.tiles;
       pos += t1 - t0;
       piece(rq, b, head, rt, t0, t1);
@@ -447,7 +448,7 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
   const int64_t job = (int64_t)blockIdx.x * kRowsPerGroup + (kJoin == 1 ? wave : 0);
   if (job >= (int64_t)p.n_rows * p.hq) return;
   const int row = (int)(job / p.hq), h = (int)(job % p.hq);
-  Axis<R> axis(p);
+  Axis<R> axis(p, typename Axis<R>::RowsOnly{});
   const int b = axis.find_row(p, row);
   const Request rq = axis.at(p, b);
   const int i = row - rq.first;
@@ -459,9 +460,11 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
   float m = -INFINITY, l = 0.f, exact = 0.f;               // exact: of the weights before they were rounded, for the log-sum-exp
   const bool with_lse = p.lse != nullptr;
   if (rq.tiles > 0) {
-    const uint32_t share = axis.share(p);
+    const bool few = p.n_requests <= 64;
+    const uint32_t share = few ? axis.share(p) : (uint32_t)scalar_load(reinterpret_cast<const int32_t*>(p.begins), 0);
+    const uint32_t begin = few ? axis.begin_of(b) : (uint32_t)scalar_load(reinterpret_cast<const int32_t*>(p.begins), 1 + b);
     const int r = i * p.group + h % p.group, rt = r / R, row_tiles = (rq.rows + R - 1) / R;
-    const uint32_t from = axis.begin_of(b) + (uint32_t)(h / p.group * row_tiles + rt) * (uint32_t)rq.tiles;
+    const uint32_t from = begin + (uint32_t)(h / p.group * row_tiles + rt) * (uint32_t)rq.tiles;
     const int first = (int)(from / share);
     int last = (int)((from + rq.tiles - 1) / share);
     last = last < p.workgroups ? last : p.workgroups - 1;

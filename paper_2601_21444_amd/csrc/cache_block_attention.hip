@@ -87,6 +87,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_ker
     const uint32_t rel = pos - begin, item = rel / (uint32_t)rq.tiles;
     const int head = (int)(item / (uint32_t)row_tiles), rt = (int)(item - (uint32_t)head * row_tiles);
     const int t0 = (int)(rel - item * (uint32_t)rq.tiles);
+    if (rel == 0 && wave == 0) axis.leave_word(p, b, begin, share);
     const int t1 = end - pos < (uint32_t)(rq.tiles - t0) ? t0 + (int)(end - pos) : rq.tiles;
     pos += t1 - t0;
 

@@ -66,8 +66,8 @@ struct Axis {
   uint32_t base_begin;       // where the window begins on the axis
   Request mine;
   uint32_t past;             // where `mine` ends
-  int per, group_first;      // this lane's group: its first query row ...
-  uint32_t group_past;      // ... and where it ends
+  int per, group_first;      // this lane's group: its first query row (RowsOnly) ...
+  uint32_t group_past;       // ... and where it ends
 
   __device__ __forceinline__ static uint32_t top(uint32_t x) { return x < 0x7fff0000u ? x : 0x7fff0000u; }
   __device__ __forceinline__ static uint32_t tiles(const CacheAttnParams& p, const Request& r) {
@@ -93,7 +93,6 @@ struct Axis {
     }
     const int lane = threadIdx.x & 63;
     per = (p.n_requests + 63) / 64;
-    group_first = 0x7fffffff;
     uint32_t sum = 0;
     for (int u = 0; u < per; u += 4) {
       Request r[4];
@@ -102,13 +101,32 @@ struct Axis {
         const int b = lane * per + u + v;
         r[v] = load(p, b < p.n_requests ? b : p.n_requests - 1);
         if (u + v >= per || b >= p.n_requests) r[v].rows = 0;
-        else if (u + v == 0) group_first = r[v].first;
       }
 #pragma unroll
       for (int v = 0; v < 4; ++v) sum = add_sat(sum, tiles(p, r[v]));
     }
     group_past = wave_scan(sum);
     total = top(__builtin_amdgcn_readlane(group_past, 63));
+  }
+  // Of the rows alone, for find_row: whoever takes a request's first tile leaves word of where it begins.
+  struct RowsOnly {};
+  __device__ __forceinline__ Axis(const CacheAttnParams& p, RowsOnly) {
+    if (p.n_requests <= 64) {
+      window(p, 0, 0);
+      total = top(__builtin_amdgcn_readlane(past, 63));
+      return;
+    }
+    per = (p.n_requests + 63) / 64;
+    const int b = (int)(threadIdx.x & 63) * per;
+    group_first = 0x7fffffff;
+    if (b < p.n_requests) group_first = clip(p.starts ? p.starts[b] : b * p.each, p.n_rows);
+    group_past = 0;
+  }
+  __device__ __forceinline__ void leave_word(const CacheAttnParams& p, int b, uint32_t begin, uint32_t share) const {
+    if (p.n_requests > 64 && (threadIdx.x & 63) == 0) {
+      p.begins[1 + b] = begin;
+      if (begin == 0) p.begins[0] = share;
+    }
   }
   __device__ __forceinline__ void group_window(const CacheAttnParams& p, int group) {
     window(p, group * per, group > 0 ? __builtin_amdgcn_readlane(group_past, group - 1) : 0);

@@ -141,10 +141,11 @@ struct CachePlan {
 // keys, 17 or 20 tiles a share: 18.7 / 18.1; of 5 or 8, 40000 keys: 13.0 / 14.1; 64 requests, 57 or 60: 51.7 / 52.5).
 //
 // Where the table holds but a few tiles a request, a workgroup takes a whole (request, KV head, row tile): no axis to plan, no
-// parts, no second launch.  It is alone with its keys, so a table of longer requests, or one of 2048 tokens where there are few,
-// is cut as above (us, cut / whole, one query each, 16 / 2 heads of 128): 1 request of 64 keys 8.2 / 4.5, 700 10.9 / 8.4, 1024 10.9 /
-// 9.6, 2048 11.6 / 13.9; 32 requests of up to 2048 15.4 / 14.2; 256 of up to 1024 24.4 / 15.2, 2048 29.4 / 22.2, 4096 37.0 / 37.1;
-// 256 of 300 to 2048 keys, 5 to 8 queries, 8 / 2 heads of 64 35.7 / 17.4; 64 of 512 to 8192, 28 / 4 heads 29.8 / 42.6.
+// parts, no second launch.  It is alone with its keys, so a table of longer requests is cut as above unless there are many to
+// even them out (us, cut / whole, one query each): 1 request of 700 keys, 16 / 2 heads of 128 9.6 / 7.8, 1280 9.4 / 10.3; 64 of 65 to
+// 2048 13.0 / 13.7, 128 17.0 / 14.2; 64 of 8 / 2 heads of 64 11.7 / 10.6, 256 17.6 / 13.1; 512 of up to 4096, 16 / 2 heads of 128 42.5 /
+// 45.9; 4096 of 8 / 2 heads of 64 198 / 154; 2048 of up to 8192 146 / 136, 4096 of up to 16384 414 / 452; 256 of 300 to 2048 keys, 5 to
+// 8 queries 35.7 / 17.4.
 //
 // The second launch takes a wave per row of the output, or four where the rows are few and have many parts (us for the call, one
 // wave / four: one query over 133120 keys, 16 / 2 heads of 128 24.8 / 19.6, 17 queries over 10000, 28 / 4 heads 24.4 / 22.7, 64
@@ -161,19 +162,22 @@ inline CachePlan choose_cache_plan(int n_requests, int hq, int hkv, int d, int64
   p.least_tiles = 2;
   p.share_step = few ? kCacheWaves : 1;
   const int64_t longest = (max_len + kCacheKeyTile - 1) / kCacheKeyTile;
-  p.whole = p.rows != kCacheBlockRows && (longest <= 20 || (longest <= 32 && (int64_t)n_requests * hkv * p.row_tiles >= 64));
+  p.whole = p.rows != kCacheBlockRows && (longest <= 16 || (int64_t)n_requests * hkv * p.row_tiles >= (longest <= 32 ? 4 : 64) * longest);
   const int64_t parts = p.workgroups / ((int64_t)n_requests * hkv * p.row_tiles) + 1;      // of a row, if the requests are alike
   p.join_waves = parts > 8 && n_rows * hq <= 1024 ? 4 : 1;
   return p;
 }
 inline size_t cache_part_bytes(int rows, int d) { return (size_t)rows * (size_t)(d + 3) * sizeof(float); }
+inline size_t cache_parts_bytes(const CachePlan& p, int d) {
+  const size_t heads = p.rows != 32 ? 0 : (size_t)kCacheWaves * p.rows * d * sizeof(float);      // pieces that have no room in LDS
+  return align256((size_t)p.workgroups * (2 * cache_part_bytes(p.rows, d) + heads));
+}
 inline size_t cache_attention_workspace_bytes(int n_requests, int64_t n_rows, int hq, int hkv, int d, int64_t max_q) {
   if (check_heads(1, hq, hkv, d) != APBV_OK || n_requests < 1 || n_requests > APBV_CACHE_MAX_REQUESTS || n_rows < 0 || n_rows > kMaxTokens ||
       n_rows * (hq / hkv) > (int64_t)1 << 30 || max_q < 0 || max_q > kMaxTokens)
     return 0;
   const CachePlan p = choose_cache_plan(n_requests, hq, hkv, d, n_rows, max_q, 0);
-  const size_t heads = p.rows != 32 ? 0 : (size_t)kCacheWaves * p.rows * d * sizeof(float);      // pieces that have no room in LDS
-  return align256((size_t)p.workgroups * (2 * cache_part_bytes(p.rows, d) + heads));
+  return cache_parts_bytes(p, d) + align256(((size_t)n_requests + 1) * sizeof(uint32_t));
 }
 
 }  // namespace apbv

@@ -37,8 +37,9 @@ int main() {
           CHECK(cache_attention_workspace_bytes(n, rows, h[0], h[1], d, q) >= (size_t)p.workgroups * 2 * p.rows * (d + 3) * 4);
         }
   // a workgroup for every (request, head, row tile): short tables, or rather short ones of many
-  CHECK(choose_cache_plan(1, 2, 1, 64, 1, 1, 1280).whole && !choose_cache_plan(1, 2, 1, 64, 1, 1, 1281).whole);
-  CHECK(choose_cache_plan(32, 16, 2, 128, 32, 1, 2048).whole && !choose_cache_plan(31, 16, 2, 128, 31, 1, 2048).whole && !choose_cache_plan(4096, 16, 2, 128, 4096, 1, 2049).whole);
+  CHECK(choose_cache_plan(1, 2, 1, 64, 1, 1, 1024).whole && !choose_cache_plan(1, 2, 1, 64, 1, 1, 1025).whole);
+  CHECK(choose_cache_plan(64, 16, 2, 128, 64, 1, 2048).whole && !choose_cache_plan(63, 16, 2, 128, 63, 1, 2048).whole);
+  CHECK(choose_cache_plan(4096, 8, 2, 64, 4096, 1, 8192).whole && !choose_cache_plan(4096, 8, 2, 64, 4096, 1, 8193).whole);
   CHECK(!choose_cache_plan(1, 16, 2, 128, 5, 5, 64).whole && choose_cache_plan(1, 16, 2, 128, 4, 4, 64).whole);      // more than 32 rows: shared keys
   // the axis: as many tiles as 32 bits number, and no more
   CHECK(cache_axis_fits(1, 1, 1, 1, kMaxCachedTokens) && cache_axis_fits(4096, 4096, 28, 4, 1 << 20) && !cache_axis_fits(4096, 4096, 8, 8, kMaxCachedTokens));

@@ -355,6 +355,22 @@ def test_many_requests():
     x.check(out, lse, True, "many, short")
 
 
+@pytest.mark.parametrize("n", [65, 200, 1030])
+@pytest.mark.parametrize("hq,hkv,d,most", [(2, 2, 64, 3), (8, 1, 64, 4), (6, 1, 128, 9)])      # tiles of 16, of 32 and of 128 rows
+def test_many_requests_cut_among_workgroups(n, hq, hkv, d, most):
+    """Keys cut (the table has room for long requests), requests without rows and without keys among them, then equal blocks."""
+    rng = np.random.default_rng((23, n, hq, most))
+    rows = rng.integers(0, most + 1, n)
+    rows[n // 2] = most
+    keys = np.where(rng.random(n) < 0.15, 0, rng.integers(1, 200, n))
+    x = Batch(rng, hq, hkv, d, 16, [(int(a), int(b)) for a, b in zip(rows, keys)], lead=2, tail=1)
+    out, lse = x.run(wide=True)
+    x.check(out, lse, True, f"{n} requests")
+    x = Batch(rng, hq, hkv, d, 16, [(most, int(b)) for b in keys])
+    out, lse = x.run(starts=False, wide=True)
+    x.check(out, lse, True, f"{n} requests of {most}")
+
+
 def test_peaked_logits_and_growing_keys():
     """References move along the keys; one key carries nearly all the weight."""
     for factor in (0.0, 8.0):
