@@ -4,8 +4,8 @@
 // Rows.  Four lanes share a block of 32 elements, eight each: 16 bytes of bf16 against 4 bytes of codes, for K and V at once.
 // The block's maximum is taken on the absolute bit patterns (bf16 of one sign order as integers), so its exponent field gives
 // the scale without arithmetic; the conversions are the hardware's own for this format (round to nearest even, saturating).
-// Both directions move bytes and are bound by them: 16384 tokens of 4 heads of 128 are written in 9.6 us (4.4 TB/s) and read
-// back in 6.6 (6.4 TB/s); from 64 tokens a launch's 2.5 us are all.
+// Both directions move bytes and are bound by them: 16384 tokens of 4 heads of 128 are written in 9.7 us (4.4 TB/s) and read
+// back in 7.4 (5.8 TB/s); of 64 tokens a launch's 2.5 us are all.
 //
 // Tables.  The lengths are few thousand integers: a workgroup takes their prefix sums, finds which requests are granted, and then
 // deals tokens and pages to its threads.  A hundred thousand tokens of prompts are dealt to as many workgroups as they fill, each

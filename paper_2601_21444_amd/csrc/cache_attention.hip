@@ -8,8 +8,12 @@
 // every wave an equal part of that: a batch of unequal lengths fills the chip as an equal one does, and so does one request.
 // A wave finishes the row tiles that lie in its part by itself; the pieces of others are put together in LDS at the end, and
 // what a workgroup shares with its neighbours is left in the workspace in float32 (O, maxima, row sums), where a second launch
-// joins it.  (All waves on one row tile at a time: 256 requests of 65 to 2048 keys 24.2 us instead of 16.9, 64 requests of 512 to
-// 32768 53.7 instead of 47.8, one of 133120 14.4 instead of 14.8.)
+// joins it.  (All waves on one row tile at a time took 53.7 us instead of 47.8 for 64 requests of 512 to 32768 keys, 24.2 instead
+// of 16.9 for 256 of 65 to 2048, 14.4 instead of 14.8 for one of 133120.)
+//
+// Bound by memory in batches and long requests: 64 requests, 28 / 4 heads of 128, 251 MB in 44.5 us (5.6 TB/s; the join 4.7 more),
+// one tile of 256 units more costs 1.3 us (6.9 TB/s); 133120 keys, 36 MB in 12.0 us, of which the start (lengths, page, codes, one
+// after the other) takes 3 and the end 2, the join 5.1.
 //
 // Keys.  A lane of the matrix instruction's A operand needs eight elements of one key, and which elements go with which k-step
 // is free as long as K and Q agree: lane (key li, quarter lg) takes the quarter's 16 bytes of codes, one load, all of one

@@ -129,16 +129,16 @@ struct CachePlan {
 };
 // Two workgroups fit a compute unit.  Where each would get but a few tiles, one is given the double: every share costs its start
 // and end and two parts to join (us, 512 / 256 workgroups: one query over 133120 keys, 16 / 2 heads of 128, 8.1 tiles each of
-// 512, 20.3 / 19.3; 256 requests of 65 to 2048 keys, 8 / 2 heads of 64, 9 tiles, 21.6 / 22.9; 64 queries over 16512 keys, 4 tiles,
-// 36 / 34; 64 requests of 512 to 32768 keys, 28 / 4 heads of 128, 56 tiles, 50.6 / 52.0).  Shares of one tile rather than two cost
-// the join more than they save (16000 keys 12.4 / 11.8; 64 queries over 2000 keys 21.6 / 17.4).
+// 512, 19.9 / 17.6; 256 requests of 65 to 4096 keys, 8 / 2 heads of 64, 16 tiles, 21.9 / 23.7; 64 queries over 16512 keys, 4 tiles,
+// 35.7 / 32.8; 64 requests of 512 to 32768 keys, 28 / 4 heads of 128, 56 tiles, 49.4 / 50.1).  Shares of one tile rather than two
+// cost the join more than they save (64 queries over 2000 keys 21.9 / 18.3).
 //
 // Few row tiles of 16 rows have hardly an end inside a workgroup, which a second one would fill with work: one is enough at
-// head_dim 128, however long (one query, 16 / 2 heads, 512 / 256 workgroups: 262144 keys 26.5 / 23.3, 524288 37.0 / 33.2; 64 / 8
-// heads, 400000 keys 89.5 / 86.9; with pages of 16 tokens 262144 keys 28.4 / 26.5, 500000 37.6 / 39.0), and below 12 tiles each at
-// 64 (8 / 2 heads: 133120 keys, 8 tiles each of 512, 15.1 / 13.4; 500000, 31 tiles, 23.9 / 24.6).  Their waves take equally many
-// tiles where that makes a share not much longer: the longest part is as long as before, and there are fewer to join (133120
-// keys, 17 or 20 tiles a share: 18.7 / 18.1; of 5 or 8, 40000 keys: 13.0 / 14.1; 64 requests, 57 or 60: 51.7 / 52.5).
+// head_dim 128, however long (one query, 16 / 2 heads, 512 / 256 workgroups: 262144 keys 25.0 / 22.1, 524288 34.5 / 31.8; with pages
+// of 16 tokens 500000 keys 35.0 / 33.5; 64 / 8 heads, 400000 keys 88.7 / 90.4), and below 12 tiles each at 64 (8 / 2 heads: 133120
+// keys, 8 tiles each of 512, 14.4 / 12.9; 500000, 31 tiles, 22.5 / 24.4).  Their waves take equally many tiles where that makes a
+// share not much longer: the longest part is as long as before, and there are fewer to join (133120 keys, 17 or 20 tiles a share:
+// 18.3 / 17.8; of 5 or 8, 40000 keys: 12.5 / 13.4; 64 requests, 57 or 60: 51.7 / 52.5).
 //
 // Where the table holds but a few tiles a request, a workgroup takes a whole (request, KV head, row tile): no axis to plan, no
 // parts, no second launch.  It is alone with its keys, so a table of longer requests is cut as above unless there are many to
@@ -148,9 +148,9 @@ struct CachePlan {
 // 8 queries 35.7 / 17.4.
 //
 // The second launch takes a wave per row of the output, or four where the rows are few and have many parts (us for the call, one
-// wave / four: one query over 133120 keys, 16 / 2 heads of 128 24.8 / 19.6, 17 queries over 10000, 28 / 4 heads 24.4 / 22.7, 64
-// queries over 16512, 16 / 2 heads 32.8 / 32.3; 4 x 64 queries, 8 / 2 heads of 64 19.6 / 22.7, 64 requests of one query, 28 / 4
-// heads 51.6 / 55.1).
+// wave / four: one query over 133120 keys, 16 / 2 heads of 128 22.3 / 17.9, 17 queries over 10000, 28 / 4 heads 24.4 / 23.0, 64
+// queries over 16512, 16 / 2 heads 32.8 / 32.4; 4 x 64 queries, 8 / 2 heads of 64 19.6 / 23.0, 64 requests of one query, 28 / 4
+// heads 49.6 / 52.2).
 inline CachePlan choose_cache_plan(int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q, int64_t max_len) {
   const int64_t rows = (max_q < n_rows ? max_q : n_rows) * (hq / hkv);      // at most 2^30
   CachePlan p;
