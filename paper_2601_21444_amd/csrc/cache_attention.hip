@@ -48,7 +48,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(co
 
   // per-lane LDS offsets: V rows as written, and as the A operand of O^T (query_attention.hip)
   constexpr int kPieces = D / 64 * 2;                      // 16-byte chunks of a lane's quarter row
-  auto fv = [](int r) { return T::fv(r) | (r >> 3 & 1); };             // (the bit spreads the writes of sixteen rows over all banks)
+  // (the lowest bit spreads the writes: of eight rows, which go together, over eight chunks of 128 bytes, of sixteen over all)
+  auto fv = [](int r) { return T::fv(r) | (((D == 128 ? r >> 2 : r) ^ r >> 3) & 1); };
   int v_put[kPieces], v_off[T::DBN];
 #pragma unroll
   for (int x = 0; x < kPieces; ++x) v_put[x] = li * T::ROW_BYTES + (((lg * kPieces + x) ^ fv(li)) << 4);
