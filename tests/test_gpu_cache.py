@@ -556,6 +556,27 @@ def test_a_server_that_admits_decodes_and_releases(captured):
     assert refusals >= 2 and s.count.item() == n_pages
 
 
+def test_calls_at_once_on_two_streams():
+    """Batches of both kernels, cut and joined, on two streams with a workspace each: as one after the other."""
+    rng = np.random.default_rng(31)
+    batches = [Batch(rng, 16, 2, 128, 64, [(1, 6000), (1, 300)]), Batch(rng, 8, 2, 64, 32, [(40, 3000), (70, 900)])]
+    want = [x.run() for x in batches]
+    calls = []
+    for x in batches:
+        n, most = len(x.requests), max(n for n, _ in x.requests)
+        need = apbv.apbv_cache_attention_workspace_bytes(n, x.rows, x.hq, x.hkv, x.d, most)
+        calls.append((x, dev_int(x.table.tolist()), x.lengths(), dev_int(x.starts), most, torch.empty(need, dtype=torch.uint8, device="cuda"),
+                      torch.empty((x.rows, x.hq, x.d), dtype=torch.bfloat16, device="cuda"), torch.empty((x.hq, x.rows), device="cuda")))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (x, table, lengths, starts, most, ws, out, lse), stream in zip(calls, streams):
+            apbv.apbv_cache_attention(x.q, x.cache, table, lengths, x.scale, q_starts=starts, max_q=most, out=out, lse_out=lse, workspace=ws, stream=stream)
+        torch.cuda.synchronize()
+        for (_, _, _, _, _, _, out, lse), (o, l) in zip(calls, want):
+            assert torch.equal(out, o) and torch.equal(lse, l)
+
+
 def test_two_graphs_share_a_workspace():
     """Calls ordered on one stream may share it: each replay leaves what its own call gives."""
     xs = [Batch(np.random.default_rng((15, i)), 16, 2, 128, 64, r) for i, r in enumerate(([(1, 3333)], [(1, 200), (4, 999), (1, 2048)]))]
