@@ -13,7 +13,7 @@
 //
 // Bound by memory in batches and long requests: 64 requests, 28 / 4 heads of 128, 251 MB in 44.5 us (5.6 TB/s; the join 4.7 more),
 // one tile of 256 units more costs 1.3 us (6.9 TB/s); 133120 keys, 36 MB in 12.0 us, of which the start (lengths, page, codes, one
-// after the other) takes 3 and the end 2, the join 5.1.
+// after the other) takes 3 and the end 2, the join 4.7.
 //
 // Keys.  A lane of the matrix instruction's A operand needs eight elements of one key, and which elements go with which k-step
 // is free as long as K and Q agree: lane (key li, quarter lg) takes the quarter's 16 bytes of codes, one load, all of one
@@ -477,8 +477,8 @@ __global__ __launch_bounds__(kJoin == 1 ? 256 : 64 * kJoin) void cache_join_kern
     const float* stat = part_stats(p, 0, R, D) + (int64_t)(r % R) * p.workgroups;
     const float* rows = p.parts + (r % R) * D + 4 * c;
     // a wave's equal share of the parts, kAtOnce * kLoads at a time: lane n holds the n-th's maximum and row sum, and the rows
-    // are on their way while the weights are found
-    constexpr int kLoads = 8, kChunk = kAtOnce * kLoads;
+    // are on their way while the weights are found (32 at a time where four waves join: one request of 133120 keys has 30 for each)
+    constexpr int kLoads = kJoin == 1 ? 8 : 32 / kAtOnce, kChunk = kAtOnce * kLoads;
     const int each = kJoin == 1 ? last - first + 1 : (last - first + kJoin) / kJoin;
     const int from_part = first + (kJoin == 1 ? 0 : wave * each);
     const int past_part = from_part + each <= last ? from_part + each : last + 1;
