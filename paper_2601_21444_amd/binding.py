@@ -234,6 +234,19 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     return int(stream.cuda_stream)
 
 
+def _new(shape, dtype: torch.dtype, device: torch.device, stream: Optional[torch.cuda.Stream], *, returned: bool = True) -> torch.Tensor:
+    """An output (or a workspace, not ``returned``) that the caller left to the binding.  Where the call names its stream it is that
+    stream's memory: a block of the current stream could still be in use there, and would go to the next one who asks as soon as the
+    binding lets go of it, before the call has run.  What is returned is read by the current stream, too, and kept until that is done."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned and stream != torch.cuda.current_stream(device):
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 REDUCERS = {"sum": 0, "max": 1, "softmax_sum": 2}
 
 

@@ -1,5 +1,5 @@
 """The key/value cache held in 4 bits (include/apbv_cache.h): argument marshalling only, as binding.py for include/apbv.h; the
-plain call is marshalled in native code there and here.
+plain call is marshalled in native code there and here.  What a call that names a ``stream`` allocates is memory of that stream.
 
 A serving program keeps, for all layers, the block table ``[requests, max_blocks]``, the requests' lengths and the list of free
 pages, and an :class:`ApbvCache` per layer.  A step is ``apbv_cache_map`` once, then in every layer ``apbv_cache_store`` of the
@@ -14,7 +14,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding
-from .binding import ApbvCacheStruct, ApbvError, _check_buffer, _stream_ptr, load_library, tensor_view
+from .binding import ApbvCacheStruct, ApbvError, _check_buffer, _new, _stream_ptr, load_library, tensor_view
 
 CACHE_MAX_REQUESTS = 4096      # APBV_CACHE_MAX_REQUESTS of include/apbv_cache.h
 
@@ -133,7 +133,7 @@ def apbv_cache_map(old_lengths: torch.Tensor, new_lengths: torch.Tensor, block_t
         _check_buffer(t, name, torch.int32, size, dev)
 
     def new(size):
-        return torch.empty(size, dtype=torch.int32, device=dev)
+        return _new(size, torch.int32, dev, stream)
     lengths_out = new(n) if lengths_out is None else lengths_out
     starts_out = new(n + 1) if starts_out is None else starts_out
     slots_out = new(max(max_new, 0)) if slots_out is None else slots_out
@@ -190,9 +190,9 @@ def apbv_cache_load(cache: ApbvCache, slots: torch.Tensor, *, k_out: Optional[to
     _check_buffer(k_out, "k_out", torch.bfloat16, (n, heads, d), dev)
     _check_buffer(v_out, "v_out", torch.bfloat16, (n, heads, d), dev)
     if k_out is None:
-        k_out = torch.empty((n, heads, d), dtype=torch.bfloat16, device=dev)
+        k_out = _new((n, heads, d), torch.bfloat16, dev, stream)
     if v_out is None:
-        v_out = torch.empty((n, heads, d), dtype=torch.bfloat16, device=dev)
+        v_out = _new((n, heads, d), torch.bfloat16, dev, stream)
     st = lib.apbv_cache_load(ctypes.byref(view), heads, d, n, *(t.data_ptr() if n else None for t in (slots, k_out, v_out)), _stream_ptr(stream))
     if st != 0:
         raise ApbvError(st, "apbv_cache_load")
@@ -235,11 +235,12 @@ def apbv_cache_attention(q: torch.Tensor, cache: ApbvCache, block_table: torch.T
     _check_buffer(lse_out, "lse_out", torch.float32, (hq, rows), dev)
     _check_buffer(workspace, "workspace", torch.uint8, 0, dev)
     if out is None:
-        out = torch.empty((rows, hq, d), dtype=torch.bfloat16, device=dev)
+        out = _new((rows, hq, d), torch.bfloat16, dev, stream)
     if return_lse and lse_out is None:
-        lse_out = torch.empty((hq, rows), dtype=torch.float32, device=dev)
+        lse_out = _new((hq, rows), torch.float32, dev, stream)
     if workspace is None:
-        workspace = torch.empty(max(apbv_cache_attention_workspace_bytes(n, rows, hq, heads, d, max_q), 256), dtype=torch.uint8, device=dev)
+        workspace = _new(max(apbv_cache_attention_workspace_bytes(n, rows, hq, heads, d, max_q), 256), torch.uint8, dev, stream,
+                         returned=False)
     st = lib.apbv_cache_attention(ctypes.byref(view), n, hq, heads, d, qv, block_table.data_ptr(), stride, max_blocks, lengths.data_ptr(),
                                   q_starts.data_ptr() if q_starts is not None else None, operator.index(max_q), int(bool(causal)),
                                   float(softmax_scale), out.data_ptr() if rows else None, lse_out.data_ptr() if lse_out is not None else None,
