@@ -295,16 +295,16 @@ def apbv_compress_kv(q_probe: torch.Tensor, k_local: torch.Tensor, v_local: torc
     _check_buffer(scores_out, "scores_out", torch.float64, (b, hkv, L), dev)
     _check_buffer(workspace, "workspace", torch.uint8, 0, dev)
     if idx_out is None:
-        idx_out = torch.empty((b, hkv, l_p), dtype=torch.int32, device=dev)
+        idx_out = _new((b, hkv, l_p), torch.int32, dev, stream)
     if k_c_out is None:
-        k_c_out = torch.empty((b, l_p, hkv, d), dtype=torch.bfloat16, device=dev)
+        k_c_out = _new((b, l_p, hkv, d), torch.bfloat16, dev, stream)
     if v_c_out is None:
-        v_c_out = torch.empty((b, l_p, hkv, d), dtype=torch.bfloat16, device=dev)
+        v_c_out = _new((b, l_p, hkv, d), torch.bfloat16, dev, stream)
     if return_scores and scores_out is None:
-        scores_out = torch.empty((b, hkv, L), dtype=torch.float64, device=dev)
+        scores_out = _new((b, hkv, L), torch.float64, dev, stream)
     if workspace is None:
         nbytes = max(apbv_compress_reduced_workspace_bytes(reducer, b, hq, hkv, d, q_probe.shape[-3], L, l_p), 256)
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        workspace = _new(nbytes, torch.uint8, dev, stream, returned=False)
     entry = lib.apbv_compress_kv if reducer == "sum" else lib.apbv_compress_kv_reduced
     lead = () if reducer == "sum" else (REDUCERS[reducer], float(softmax_scale))
     st = entry(
@@ -388,9 +388,9 @@ def apbv_host_attention(q_local: torch.Tensor, k_anchor: torch.Tensor, v_anchor:
     _check_buffer(out, "out", torch.bfloat16, (b, L, hq, d), dev)
     _check_buffer(lse_out, "lse_out", torch.float32, (b, hq, L), dev)
     if out is None:
-        out = torch.empty((b, L, hq, d), dtype=torch.bfloat16, device=dev)
+        out = _new((b, L, hq, d), torch.bfloat16, dev, stream)
     if return_lse and lse_out is None:
-        lse_out = torch.empty((b, hq, L), dtype=torch.float32, device=dev)
+        lse_out = _new((b, hq, L), torch.float32, dev, stream)
     st = lib.apbv_host_attention(b, hq, hkv, d, *views, float(softmax_scale), out.data_ptr(),
                                  lse_out.data_ptr() if lse_out is not None else None, _stream_ptr(stream))
     return _attention_result(st, "apbv_host_attention", q_local, out, lse_out, return_lse)
@@ -432,9 +432,9 @@ def apbv_host_attention_group(problems, softmax_scale: float, *, return_lse: boo
         _check_buffer(out, "out", torch.bfloat16, (L, hq, d), q.device)
         _check_buffer(lse, "lse_out", torch.float32, (hq, L), q.device)
         if out is None:
-            out = torch.empty((L, hq, d), dtype=torch.bfloat16, device=q.device)
+            out = _new((L, hq, d), torch.bfloat16, q.device, stream)
         if return_lse and lse is None:
-            lse = torch.empty((hq, L), dtype=torch.float32, device=q.device)
+            lse = _new((hq, L), torch.float32, q.device, stream)
         it = items[m]
         (it.q_local, it.k_anchor, it.v_anchor, it.k_pass, it.v_pass, it.k_local, it.v_local) = views
         it.out = out.data_ptr()
@@ -479,13 +479,13 @@ def apbv_query_attention(q_block: torch.Tensor, k_anchor: torch.Tensor, v_anchor
     _check_buffer(lse_out, "lse_out", torch.float32, (b, hq, n_q), dev)
     _check_buffer(workspace, "workspace", torch.uint8, 0, dev)
     if out is None:
-        out = torch.empty((b, n_q, hq, d), dtype=torch.bfloat16, device=dev)
+        out = _new((b, n_q, hq, d), torch.bfloat16, dev, stream)
     if return_lse and lse_out is None:
-        lse_out = torch.empty((b, hq, n_q), dtype=torch.float32, device=dev)
+        lse_out = _new((b, hq, n_q), torch.float32, dev, stream)
     if workspace is None:
         n_keys = k_anchor.shape[-3] + k_pass.shape[-3] + k_local.shape[-3]
         nbytes = apbv_query_attention_workspace_bytes(b, hq, d, n_q, max(n_keys, 1), n_splits)
-        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=dev)
+        workspace = _new(max(nbytes, 256), torch.uint8, dev, stream, returned=False)
     st = lib.apbv_query_attention(b, hq, hkv, d, *views, float(softmax_scale), int(n_splits), out.data_ptr(),
                                   lse_out.data_ptr() if lse_out is not None else None,
                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(),
@@ -518,9 +518,9 @@ def apbv_merge_lse(parts_out: torch.Tensor, parts_lse: torch.Tensor, *, return_l
     _check_buffer(out, "out", torch.bfloat16, (rows, hq, d), parts_out.device)
     _check_buffer(lse_out, "lse_out", torch.float32, (hq, rows), parts_out.device)
     if out is None:
-        out = torch.empty((rows, hq, d), dtype=torch.bfloat16, device=parts_out.device)
+        out = _new((rows, hq, d), torch.bfloat16, parts_out.device, stream)
     if return_lse and lse_out is None:
-        lse_out = torch.empty((hq, rows), dtype=torch.float32, device=parts_out.device)
+        lse_out = _new((hq, rows), torch.float32, parts_out.device, stream)
     st = lib.apbv_merge_lse(n, rows, hq, d, parts_out.data_ptr(), parts_out.stride(0), parts_lse.data_ptr(),
                             parts_lse.stride(0), out.data_ptr(), lse_out.data_ptr() if lse_out is not None else None,
                             _stream_ptr(stream))

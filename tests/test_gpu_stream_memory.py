@@ -68,3 +68,25 @@ def test_captured_on_a_stream_that_is_not_the_current_one():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(lse, want_lse) and torch.equal(eager[0], want), rep
+
+
+def test_prefill_calls_at_once_on_two_streams():
+    """A split query attention, its parts merged, and a compression: each with a workspace of the binding's own."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rows = lambda n, h: torch.randn((n, h, 128), generator=g, device="cuda").bfloat16()
+    none = rows(0, 2)
+    problems = [(rows(8, 16), rows(300, 2), rows(300, 2), rows(4000, 2), rows(4000, 2), none, none) for _ in range(2)]
+
+    def run(p, **kw):
+        parts = [apbv.apbv_query_attention(*p[:3], none, none, none, none, 0.1, return_lse=True, **kw),
+                 apbv.apbv_query_attention(p[0], none, none, *p[3:], 0.1, n_splits=9, return_lse=True, **kw)]
+        return parts[0] + parts[1] + apbv.apbv_compress_kv(*p[:1], *p[3:5], 100, return_scores=True, **kw)
+    want = [run(p) for p in problems]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    print("prefill on two streams", flush=True)
+    for _ in range(5):
+        got = [run(p, stream=s) for p, s in zip(problems, streams)]
+        for s in streams:
+            torch.cuda.current_stream().wait_stream(s)
+        assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))

@@ -76,3 +76,20 @@ def test_of_the_cache(allocations):
     allocations.clear()
     apbv.apbv_cache_attention(q, c, i(3, 2), i(3), 0.1, return_lse=True, stream=CURRENT)      # nothing to tell the current stream
     assert len(allocations) == 3 and not any(m[2] for m in allocations)
+
+
+def test_of_the_prefill(allocations):
+    rows = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    prob = (rows(5, 4, 64),) + tuple(rows(n, 2, 64) for n in (3, 3, 4, 4, 5, 5))
+    empty = (rows(0, 2, 64),) * 2
+
+    def calls(call, outputs, workspaces):
+        allocations.clear()
+        call()
+        check(allocations, outputs, workspaces)
+    calls(lambda: apbv.apbv_compress_kv(rows(3, 4, 64), *prob[5:], 2, return_scores=True, stream=SIDE), 4, 1)
+    calls(lambda: apbv.apbv_compress_kv(rows(3, 4, 64), *prob[5:], 2, reducer="max", softmax_scale=0.1, stream=SIDE), 3, 1)
+    calls(lambda: apbv.apbv_host_attention(*prob, 0.1, return_lse=True, stream=SIDE), 2, 0)
+    calls(lambda: apbv.apbv_host_attention_group([prob, prob], 0.1, return_lse=True, stream=SIDE), 4, 0)
+    calls(lambda: apbv.apbv_query_attention(*prob[:5], *empty, 0.1, return_lse=True, stream=SIDE), 2, 1)
+    calls(lambda: apbv.apbv_merge_lse(rows(2, 5, 4, 64), torch.zeros(2, 4, 5), return_lse=True, stream=SIDE), 2, 0)
