@@ -145,11 +145,7 @@ struct Axis {
   }
   // Length of a workgroup's share.
   __device__ __forceinline__ uint32_t share(const CacheAttnParams& p) const {
-    uint32_t q = (total + (uint32_t)p.workgroups - 1) / (uint32_t)p.workgroups;
-    if (q < (uint32_t)p.short_tiles) q = (total + (uint32_t)p.workgroups / 2 - 1) / ((uint32_t)p.workgroups / 2);
-    q = q > (uint32_t)p.least_tiles ? q : (uint32_t)p.least_tiles;
-    if (q > 3 * (uint32_t)p.share_step) q = (q + (uint32_t)p.share_step - 1) / (uint32_t)p.share_step * (uint32_t)p.share_step;
-    return q;
+    return cache_share(total, (uint32_t)p.workgroups, (uint32_t)p.short_tiles, (uint32_t)p.least_tiles, (uint32_t)p.share_step);
   }
   // The share of this workgroup, or -1: consecutive shares on one XCD (row tiles of a head read the same keys), which a launch
   // gives its workgroups in turn.

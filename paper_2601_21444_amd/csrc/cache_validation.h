@@ -167,6 +167,14 @@ inline CachePlan choose_cache_plan(int n_requests, int hq, int hkv, int d, int64
   p.join_waves = parts > 8 && n_rows * hq <= 1024 ? 4 : 1;
   return p;
 }
+// Tiles of a workgroup's share of an axis of `total` tiles.
+constexpr uint32_t cache_share(uint32_t total, uint32_t workgroups, uint32_t short_tiles, uint32_t least_tiles, uint32_t share_step) {
+  uint32_t q = (total + workgroups - 1) / workgroups;
+  if (q < short_tiles) q = (total + workgroups / 2 - 1) / (workgroups / 2);
+  q = q > least_tiles ? q : least_tiles;
+  if (q > 3 * share_step) q = (q + share_step - 1) / share_step * share_step;
+  return q;
+}
 inline size_t cache_part_bytes(int rows, int d) { return (size_t)rows * (size_t)(d + 3) * sizeof(float); }
 inline size_t cache_parts_bytes(const CachePlan& p, int d) {
   const size_t heads = p.rows != 32 ? 0 : (size_t)kCacheWaves * p.rows * d * sizeof(float);      // pieces that have no room in LDS
