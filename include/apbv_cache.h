@@ -28,7 +28,8 @@ extern "C" {
 
 /* A pool of pages of page_size tokens (16, 32, 64, 128 or 256).  Inside a page codes are [n_kv_heads, page_size, head_dim / 2]
  * bytes and scales [n_kv_heads, page_size, head_dim / 32] bytes, both dense; pages are page_stride_* BYTES apart (multiples
- * of 16), so the pages of several layers, or K and V, may be interleaved in one allocation.  Pointers are 16-byte aligned.
+ * of 16, below 2^31), so the pages of several layers, or K and V, may be interleaved in one allocation.  Pointers are 16-byte
+ * aligned; a page holds at most 2^30 bytes of codes.
  * The slot of a token is page * page_size + its place in the page; n_pages * page_size < 2^31.  Contents need no
  * initialisation: slots that no visible key of a request names are never part of a result. */
 typedef struct {
@@ -90,8 +91,8 @@ apbv_status apbv_cache_store(const apbv_cache* cache, int n_kv_heads, int head_d
 apbv_status apbv_cache_load(const apbv_cache* cache, int n_kv_heads, int head_dim, int64_t tokens,
                             const int32_t* slots, void* k_out, void* v_out, void* hip_stream);
 
-/* Host, pure.  Bytes of workspace apbv_cache_attention needs (0 on invalid arguments); 256-byte aligned.  n_rows = q.tokens,
- * max_q as passed to the call. */
+/* Host, pure.  Bytes of workspace apbv_cache_attention needs (0 on invalid arguments; a call may still be larger than what is
+ * supported, which it says itself); 256-byte aligned.  n_rows = q.tokens, max_q as passed to the call. */
 size_t apbv_cache_attention_workspace_bytes(int n_requests, int64_t n_rows, int n_q_heads, int n_kv_heads, int head_dim,
                                             int64_t max_q);
 

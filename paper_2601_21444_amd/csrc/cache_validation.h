@@ -85,7 +85,7 @@ inline apbv_status validate_cache_load(const apbv_cache* cache, int hkv, int d, 
 // The tiles of all (request, KV head, row tile) are numbered in 32 bits; the host knows the most there can be.
 constexpr int kCacheKeyTile = 64;
 inline bool cache_axis_fits(int64_t n_requests, int64_t n_rows, int hq, int hkv, int64_t max_len) {
-  const int64_t row_tiles = (n_rows * (hq / hkv) / 16 + n_requests) * hkv;               // below 2^27 * 2^16
+  const int64_t row_tiles = (n_rows * (hq / hkv) / 16 + n_requests) * hkv;               // below 2^37 (2^24 tokens of 65535 query heads)
   return row_tiles <= (int64_t)0x7fff0000 / ((max_len + kCacheKeyTile - 1) / kCacheKeyTile);
 }
 
