@@ -105,19 +105,22 @@ size_t apbv_cache_attention_workspace_bytes(int n_requests, int64_t n_rows, int 
  * (causal == 0: a partial result, to be merged by apbv_merge_lse, whose layouts out and lse_out have).
  *
  *   q            [n_rows, n_q_heads, head_dim], any number of rows (0: nothing is done)
- *   block_table  [n_requests, max_blocks] int32, rows table_stride elements apart; entries beyond a request's keys are not read
+ *   block_table  [n_requests, max_blocks] int32, rows table_stride elements apart; entries beyond a request's keys are not read.  How
+ *                wide it is decides how the work is cut, as the host knows no lengths: the columns that are needed, of a wider table,
+ *                are faster for short requests (256 of up to 2048 keys 13 us, in a table of 131072 tokens 18)
  *   lengths      [n_requests] int32; outside [0, max_blocks * page_size] the nearest in it is taken
  *   q_starts     [n_requests + 1] int32, not descending, within [0, n_rows] (cut off there); or NULL: every request has
  *                n_rows / n_requests rows
- *   max_q        the largest number of rows of a request, or more: a question of speed and workspace only
+ *   max_q        the largest number of rows of a request, or more: a question of speed and workspace only (above 32 rows per KV head
+ *                every request is worked on in tiles of 128: 256 requests of one query 13 us with max_q = 1, 32 with 256)
  *   out          [n_rows, n_q_heads, head_dim] bf16, dense;  lse_out optional (may be NULL) [n_q_heads, n_rows] fp32
  * Rows of no request (before q_starts[0], behind q_starts[n_requests]) are left as they were.  A row that sees no key gets
  * zeros and -inf.  Keys on a page outside [0, n_pages) are taken as not there.
  *
  * Arithmetic: the cached values are exact in bf16; bf16 operands, fp32 accumulation and softmax, probabilities rounded to
  * bf16 before the product with V and divided by their rounded sum (the lse is of their exact one), the parts of a row that
- * several workgroups share are kept and joined in fp32, output rounded to bf16.  How the keys are cut depends on the shape of the call and on all lengths; results of the same call are
- * repeatable.
+ * several workgroups share are kept and joined in fp32, output rounded to bf16.  How the keys are cut depends on the shape of the
+ * call and on all lengths; results of the same call are repeatable.
  * Supported: head_dim in {64, 128}; n_q_heads % n_kv_heads == 0; 1 <= n_requests <= 4096; max_blocks * page_size <= 2^30;
  * n_rows * G <= 2^30; (n_rows * G / 16 + n_requests) * n_kv_heads * (max_blocks * page_size / 64) below 2^31 (a table of
  * 4096 rows for 2^20 tokens, with 8 KV heads); n_rows * n_q_heads <= 2^26 - 4; n_requests * n_kv_heads below 2^24.

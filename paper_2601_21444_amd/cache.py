@@ -209,8 +209,8 @@ def apbv_cache_attention(q: torch.Tensor, cache: ApbvCache, block_table: torch.T
                          workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Attention of the rows ``q [rows, Hq, d]`` of many requests over their cached keys; see apbv_cache_attention in
     include/apbv_cache.h.  Without ``q_starts`` every request has ``rows / requests`` rows (one: a decoding step); with it and
-    without ``max_q`` a request is taken to have up to all of them.  Returns ``out [rows, Hq, d]`` bf16 (and ``lse [Hq, rows]``
-    fp32), the layouts of apbv_merge_lse."""
+    without ``max_q`` a request is taken to have up to all of them, which takes single tokens two to three times as long.  Returns
+    ``out [rows, Hq, d]`` bf16 (and ``lse [Hq, rows]`` fp32), the layouts of apbv_merge_lse."""
     lib = load_library()
     if stream is None and type(cache) is ApbvCache and out is not None and workspace is not None and not (return_lse and lse_out is None):
         st = binding._native.cache_attention(q, cache, block_table, lengths, softmax_scale, q_starts, max_q, causal, out, lse_out, workspace)

@@ -11,7 +11,8 @@
 // deals tokens and pages to its threads.  A hundred thousand tokens of prompts are dealt to as many workgroups as they fill, each
 // of which takes the sums for itself; in place, where one would write what another has yet to read, one workgroup does all but
 // the slots, which a second launch finds.  Bound by the chain of launch, lengths, prefix sums and pages: 64 requests of one token
-// 3.9 us, of which a launch that only reads and writes takes 2.5; 48 prompts of 80000 tokens 6.6, in place 12.0.
+// 3.9 us, of which a launch that only reads and writes takes 2.5; 48 prompts of 80000 tokens 6.6, in place 12.0 (pages taken, slots and
+// pages given back each wait for memory by themselves).
 #include "cache.h"
 
 namespace apbv {
@@ -182,8 +183,9 @@ __device__ __forceinline__ int slot_of(int page, int pos, int page_log2) {
 // A thread holds kPer consecutive requests in registers and knows, after the prefix sums, where their tokens and
 // pages lie.  In a decoding step, where no request grows by more than kFew tokens, that is all it takes: every thread serves
 // its own requests.  Otherwise, and for pages given back, tokens and pages are dealt to the threads, which find the request of
-// each in LDS.  Pages are taken from where the list has them or will have them, so that nothing written here is read here: two
-// waits for memory in all, for the lengths and for the pages.
+// each in LDS, in a loop for the pages taken, one for the slots and one for the pages given back.  Pages are taken from where the list
+// has them or will have them, so that nothing written here is read here: in a decoding step two waits for memory, for the lengths and
+// for the pages (and one more if pages are given back), otherwise one for the lengths and one or more in each loop.
 template <int kPer>
 __global__ __launch_bounds__(kMapThreads) void cache_map_kernel(const CacheMapParams p, const int with_slots) {
   constexpr int kMost = kPer * kMapThreads, kWaves = kMapThreads / 64;

@@ -11,9 +11,14 @@
 // joins it.  (All waves on one row tile at a time took 53.7 us instead of 47.8 for 64 requests of 512 to 32768 keys, 24.2 instead
 // of 16.9 for 256 of 65 to 2048, 14.4 instead of 14.8 for one of 133120.)
 //
-// Bound by memory in batches and long requests: 64 requests, 28 / 4 heads of 128, 251 MB in 44.5 us (5.6 TB/s; the join 4.7 more);
-// of one request every 8192 keys of 16 / 2 heads of 128 cost 0.33 us more (6.8 TB/s); 133120 keys, 36 MB in 11.7 us, of which the
-// start (lengths, page, codes, one after the other) takes 3 and the end 2, the join 4.7.
+// Bound by memory in batches and long requests (called again and again, whose keys are partly in the last-level cache): 64 requests,
+// 28 / 4 heads of 128, 251 MB in 44.0 us (5.7 TB/s; the join 4.8 more); of one request every 8192 keys of 16 / 2 heads of 128 cost
+// 0.33 us more (6.8 TB/s); 133120 keys, 36 MB in 12.3 us, of which the start (lengths, page, codes, one after the other) takes 3 and
+// the end 2, the join 4.8.
+//
+// Weights are rounded to bf16 for the product with V, which keeps the bf16 matrix instruction at one product a key: half a step each,
+// 2^-8 at most and 1.7e-3 in root mean square.  Outputs lie 2.3e-3 from those of 64 bits where the rounding of the output alone leaves
+// 1.65e-3; two products of a weight's halves would take that away for as many matrix instructions again.
 //
 // Keys.  A lane of the matrix instruction's A operand needs eight elements of one key, and which elements go with which k-step
 // is free as long as K and Q agree: lane (key li, quarter lg) takes the quarter's 16 bytes of codes, one load, all of one

@@ -6,12 +6,15 @@
 // instructions of the tiles before it; codes are asked for a tile before they are converted.  One barrier a tile.  Every wave
 // owns its rows, so a piece of a row tile needs no joining inside the workgroup.  Matrix instruction and operands are those of
 // packed_attention.hip: with one workgroup a unit a wave has its SIMD to itself, where vector instructions are free beside
-// 32x32x16 and not beside 16x16x32.
+// 32x32x16 and not beside 16x16x32.  Weights are rounded to bf16 for the product with V, as in all attention here
+// (cache_attention.hip).
 //
-// Chunks of prompts are bound by power (1020 TFLOP/s at 1.95 GHz; a kernel of 16x16x32 instructions, and one whose waves took K
-// from memory each for itself, run at the same rate to a percent: 4 x 512 queries of 28 / 4 heads of 128 over 20000 keys 568, 568,
-// 574 us), short blocks by their start (4 us), the end (3 us) and 3000 cycles a tile of a lone wave, of which 1024 are matrix
-// instructions.
+// Chunks of prompts, two waves a SIMD, are bound by what a SIMD issues: matrix instructions are under way in 49 % of the cycles, vector
+// instructions (exponentials, conversions of keys and of weights, maxima) in 41 % more, and little of the one runs beside the other
+// (1020 TFLOP/s at 2.03 GHz; a kernel of 16x16x32 instructions, and one whose waves took K from memory each for itself, which convert
+// as much or more, run at the same rate to a percent: 4 x 512 queries of 28 / 4 heads of 128 over 20000 keys 568, 568, 574 us).
+// Every row tile of a head converts its keys again.  Short blocks are bound by their start (4 us), the end (3 us) and 3000 cycles a
+// tile of a lone wave, of which 1024 are matrix instructions.
 #include "cache_tiles.h"
 
 namespace apbv {
