@@ -33,3 +33,8 @@ from .cache import (  # noqa: F401
     apbv_cache_map,
     apbv_cache_store,
 )
+from .positions import (  # noqa: F401
+    ApbvRotation,
+    apbv_cache_append,
+    apbv_rotate,
+)

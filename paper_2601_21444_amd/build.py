@@ -29,6 +29,8 @@ SOURCES = {
     "compress.hip": [],
     "merge.hip": [],
     "packed_attention.hip": ["-fno-honor-nans"],
+    "positions.hip": [],
+    "positions_api.hip": [],
     "query_attention.hip": ["-fno-honor-nans"],
     "score_matrix.hip": [],
 }
