@@ -38,3 +38,7 @@ from .positions import (  # noqa: F401
     apbv_cache_append,
     apbv_rotate,
 )
+from .shared import (  # noqa: F401
+    apbv_cache_shared_attention,
+    apbv_cache_shared_attention_workspace_bytes,
+)

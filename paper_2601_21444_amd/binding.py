@@ -173,6 +173,15 @@ def load_library() -> ctypes.CDLL:
     lib.apbv_cache_append.argtypes = [
         ctypes.POINTER(ApbvCacheStruct), ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ApbvTensor, ApbvTensor, ApbvTensor,
         ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+    lib.apbv_cache_shared_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.apbv_cache_shared_attention_workspace_bytes.argtypes = [
+        ctypes.c_int, ctypes.c_int, ctypes.c_int64, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int64]
+    lib.apbv_cache_shared_attention.restype = ctypes.c_int
+    lib.apbv_cache_shared_attention.argtypes = [
+        ctypes.POINTER(ApbvCacheStruct), ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ApbvTensor,
+        ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p,
+        ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int,
+        ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
     _native = _load_marshal(lib)
     _lib = lib
     return lib

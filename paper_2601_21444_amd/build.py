@@ -33,6 +33,8 @@ SOURCES = {
     "positions_api.hip": [],
     "query_attention.hip": ["-fno-honor-nans"],
     "score_matrix.hip": [],
+    "shared_api.hip": [],
+    "shared_attention.hip": ["-fno-honor-nans"],
 }
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -85,14 +85,15 @@ def _check_ints(t: torch.Tensor, name: str, shape, device: torch.device) -> None
         raise ValueError(f"{name}: must be contiguous")
 
 
-def _check_table(t: torch.Tensor, n: int, device: torch.device):
+def _check_table(t: torch.Tensor, n: int, device: torch.device, name: str = "block_table"):
     """Table [n, max_blocks] -> (stride of a row, max_blocks)."""
     if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32:
-        raise TypeError(f"block_table: expected a {torch.int32} tensor")
+        raise TypeError(f"{name}: expected a {torch.int32} tensor")
     if not t.is_cuda or t.device != device:
-        raise ValueError(f"block_table: must live on {device}")
+        raise ValueError(f"{name}: must live on {device}")
     if t.dim() != 2 or t.shape[0] != n or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("block_table: expected [requests, max_blocks], blocks contiguous")
+        raise ValueError(f"{name}: expected [{n}, blocks], blocks contiguous" if name != "block_table" else
+                         "block_table: expected [requests, max_blocks], blocks contiguous")
     return t.stride(0), t.shape[1]
 
 

@@ -60,6 +60,11 @@ struct CacheAttnParams {
   int hq, hkv, group, causal;
   int workgroups, short_tiles, least_tiles, share_step;
   int row_tiles;           // of a request, by max_q
+  // of requests behind shared prefixes (shared_attention.hip): the axis of the prefixes has groups in place of requests, and row
+  // tiles that one workgroup has to itself are kept, too: [n_rows, Hq, d], then [3][n_rows, Hq] as the parts' statistics
+  const int32_t* members;  // [groups + 1]: the first request of each, or nullptr: every group has members_each
+  float* kept;
+  int n_members, members_each;      // requests of all groups, of each (more than 0; 0: no axis of groups)
   float scale_log2;        // softmax_scale * log2(e)
   double per_group;        // 1 / group
 };

@@ -55,11 +55,20 @@ __device__ __forceinline__ float log_sum(float m, float l) {
 __device__ __forceinline__ float* part_stats(const CacheAttnParams& p, int slot, int R, int D) {
   return p.parts + (int64_t)p.workgroups * 2 * (R * D) + (int64_t)slot * (3 * R) * p.workgroups;
 }
+// ... and of a row that is kept whole, the at-th of [n_rows, Hq].
+template <int D, bool kLse>
+__device__ __forceinline__ void keep_stats(const CacheAttnParams& p, int64_t at, float m, float l, float exact) {
+  const int64_t n = (int64_t)p.n_rows * p.hq;
+  float* stat = p.kept + n * D + at;
+  stat[0] = m;
+  stat[n] = l;
+  if (kLse) stat[2 * n] = exact;
+}
 
 // The axis of tiles: its length, and where the requests lie on it.  A wave holds a window of 64 consecutive requests, one a
 // lane, handed from lane to lane as they are needed; with more than 64 it first adds up 64 groups of `per` (at most 64).
 // The host has seen that the tiles of requests which do not overlap fit 32 bits; sums stop at the largest number otherwise.
-template <int R>
+template <int R, bool kGroups = false>
 struct Axis {
   uint32_t total;
   int base;                  // the window: request base + lane is `mine`
@@ -73,8 +82,13 @@ struct Axis {
   __device__ __forceinline__ static uint32_t tiles(const CacheAttnParams& p, const Request& r) {
     return (uint32_t)((r.rows + R - 1) / R * p.hkv) * (uint32_t)r.tiles;
   }
+  __device__ __forceinline__ static int first_row(const CacheAttnParams& p, int b) {
+    if constexpr (kGroups)
+      if (p.members_each > 0) b = p.members ? clip(p.members[b], p.n_members) : b * p.members_each;      // a group's first request
+    return p.starts ? p.starts[b] : b * p.each;
+  }
   __device__ __forceinline__ static Request load(const CacheAttnParams& p, int b) {
-    const int first = p.starts ? p.starts[b] : b * p.each, past_row = p.starts ? p.starts[b + 1] : (b + 1) * p.each;
+    const int first = first_row(p, b), past_row = first_row(p, b + 1);
     return request_of(p, first, past_row, p.lengths[b]);
   }
   __device__ __forceinline__ void window(const CacheAttnParams& p, int from, uint32_t begin) {
@@ -119,11 +133,12 @@ struct Axis {
     per = (p.n_requests + 63) / 64;
     const int b = (int)(threadIdx.x & 63) * per;
     group_first = 0x7fffffff;
-    if (b < p.n_requests) group_first = clip(p.starts ? p.starts[b] : b * p.each, p.n_rows);
+    if (b < p.n_requests) group_first = clip(first_row(p, b), p.n_rows);
     group_past = 0;
   }
+  template <bool kAlways = false>
   __device__ __forceinline__ void leave_word(const CacheAttnParams& p, int b, uint32_t begin, uint32_t share) const {
-    if (p.n_requests > 64 && (threadIdx.x & 63) == 0) {
+    if ((kAlways || p.n_requests > 64) && (threadIdx.x & 63) == 0) {
       p.begins[1 + b] = begin;
       if (begin == 0) p.begins[0] = share;
     }
@@ -143,15 +158,16 @@ struct Axis {
     r.tiles = __builtin_amdgcn_readlane(mine.tiles, b - base);
     return r;
   }
-  // Length of a workgroup's share.
-  __device__ __forceinline__ uint32_t share(const CacheAttnParams& p) const {
-    return cache_share(total, (uint32_t)p.workgroups, (uint32_t)p.short_tiles, (uint32_t)p.least_tiles, (uint32_t)p.share_step);
+  // Length of a workgroup's share, of as many as there are.
+  __device__ __forceinline__ uint32_t share(const CacheAttnParams& p, uint32_t workgroups) const {
+    return cache_share(total, workgroups, (uint32_t)p.short_tiles, (uint32_t)p.least_tiles, (uint32_t)p.share_step);
   }
+  __device__ __forceinline__ uint32_t share(const CacheAttnParams& p) const { return share(p, (uint32_t)p.workgroups); }
   // The share of this workgroup, or -1: consecutive shares on one XCD (row tiles of a head read the same keys), which a launch
   // gives its workgroups in turn.
-  __device__ __forceinline__ int my_share(uint32_t share) const {
+  __device__ __forceinline__ int my_share(uint32_t share, uint32_t block) const {
     const int n = (int)((total + share - 1) / share), per_xcd = (n + kXcds - 1) / kXcds;
-    const int x = (int)blockIdx.x / kXcds, wg = (int)(blockIdx.x % kXcds) * per_xcd + x;
+    const int x = (int)block / kXcds, wg = (int)(block % kXcds) * per_xcd + x;
     return x < per_xcd && wg < n ? wg : -1;
   }
   // The request that holds tile `pos` < total.
