@@ -2,7 +2,8 @@
 // current stream, the call.  For the smallest problems the interpreter's time is the call's (one launch takes 2.9 us to
 // enqueue; a call from Python took 3.4 us more for a merge, 7 to 8 us more for an attention).  Enqueueing, before / now
 // (us): merge 6.9 / 3.4, attention 10.5 / 4.8, query attention (two launches) 16.0 / 8.1, compression (three) 15.7 / 8.3; of the
-// cache's calls attention (two) 15.9 / 5.6, map 9.7 / 3.5, load 10.3 / 3.2.
+// cache's calls attention (two) 15.9 / 5.6, map 9.7 / 3.5, load 10.3 / 3.2.  Of the positions, rotate 9.8 / 3.5, append 10.8 /
+// 4.0, and shared attention (two launches) 18.3 / 6.4.
 //
 // Every function returns the call's status, or None where a call is not the plain case -- an output left to the binding to
 // allocate, an argument of another type, a tensor subclass, any check that fails: the binding then goes the general way,
@@ -12,6 +13,8 @@
 #include <vector>
 #include "apbv.h"
 #include "apbv_cache.h"
+#include "apbv_positions.h"
+#include "apbv_shared.h"
 
 namespace {
 
@@ -421,6 +424,135 @@ PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
   });
 }
 
+// ---- positions (apbv_positions.h)
+
+// A rotation as its Python object has it ready: (address of its apbv_rotation, axes, head_dim, GPU).  The object is an argument of the
+// binding's call, so it and its tensors live while this runs.
+struct RotationPlan {
+  const apbv_rotation* rotation;
+  int64_t axes, d, device;
+};
+bool rotation_of(PyObject* o, RotationPlan& r) {
+  if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 4) return false;
+  int64_t address;
+  if (!whole(PyTuple_GET_ITEM(o, 0), address) || !whole(PyTuple_GET_ITEM(o, 1), r.axes) || !whole(PyTuple_GET_ITEM(o, 2), r.d) || !whole(PyTuple_GET_ITEM(o, 3), r.device))
+    return false;
+  r.rotation = reinterpret_cast<const apbv_rotation*>(address);
+  return address != 0;
+}
+// [tokens] or [axes or more, tokens], tokens contiguous.
+bool positions_of(PyObject* o, int64_t axes, int64_t tokens, c10::Device device, const int32_t*& ptr, int64_t& stride) {
+  const at::Tensor* t = plain(o);
+  if (t == nullptr || t->scalar_type() != at::kInt || !t->is_cuda() || t->device() != device) return false;
+  const int64_t dim = t->dim();
+  if ((dim != 1 && dim != 2) || t->size(dim - 1) != tokens || (dim == 2 && t->size(0) < axes) || (tokens > 1 && t->stride(dim - 1) != 1)) return false;
+  ptr = static_cast<const int32_t*>(t->data_ptr());
+  stride = dim == 2 ? t->stride(0) : 0;
+  return true;
+}
+
+// rotate(q, k, positions, rotation, q_out, k_out); q or k (with its output) may be None
+PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (count != 6) return not_taken();
+  return guarded([&](int& status) {
+    RotationPlan r;
+    if (!rotation_of(a[3], r) || (a[0] == Py_None && a[1] == Py_None)) return false;
+    Tensor t[2];
+    void *out[2] = {nullptr, nullptr}, *stream;
+    apbv_tensor views[2] = {};
+    int64_t tokens = -1, heads[2] = {0, 0};
+    c10::Device device = at::kCPU;
+    for (int i = 0; i < 2; ++i) {
+      if (a[i] == Py_None) continue;
+      if (!view_of(a[i], t[i], 3) || t[i].d != r.d || t[i].device.index() != r.device || !t[i].device.is_cuda() || a[4 + i] == Py_None) return false;
+      if (tokens >= 0 && (t[i].tokens != tokens || t[i].device != device)) return false;
+      tokens = t[i].tokens;
+      device = t[i].device;
+      heads[i] = t[i].heads;
+      views[i] = t[i].view;
+      if (!buffer(a[4 + i], at::kBFloat16, tokens * heads[i] * r.d, device, false, out[i])) return false;
+    }
+    const int32_t* positions;
+    int64_t stride;
+    if (tokens == 0 || !positions_of(a[2], r.axes, tokens, device, positions, stride) || !current_stream(stream, &device)) return false;
+    Py_BEGIN_ALLOW_THREADS
+    status = apbv_rotate(to_int(heads[0]), to_int(heads[1]), to_int(r.d), r.rotation, views[0], views[1], positions, stride, out[0], out[1], stream);
+    Py_END_ALLOW_THREADS
+    return true;
+  });
+}
+
+// cache_append(cache, q, k, v, slots, positions, rotation, q_out); q (with q_out) may be None
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (count != 8) return not_taken();
+  return guarded([&](int& status) {
+    Cache c;
+    RotationPlan r;
+    Tensor q = {}, k, v;
+    int32_t* slots;
+    const int32_t* positions;
+    int64_t stride;
+    void *q_out = nullptr, *stream;
+    if (!cache_of(a[0], c) || !rotation_of(a[6], r) || r.d != c.d || r.device != c.device.index()) return false;
+    if (!view_of(a[2], k, 3) || !view_of(a[3], v, 3) || k.device != c.device || v.device != c.device) return false;
+    if (k.heads != c.heads || v.heads != c.heads || k.d != c.d || v.d != c.d || v.tokens != k.tokens || k.tokens == 0) return false;
+    if (a[1] != Py_None) {
+      if (!view_of(a[1], q, 3) || q.device != c.device || q.d != c.d || q.tokens != k.tokens || a[7] == Py_None ||
+          !buffer(a[7], at::kBFloat16, q.tokens * q.heads * q.d, c.device, false, q_out))
+        return false;
+    }
+    if (!ints(a[4], k.tokens, c.device, slots) || !positions_of(a[5], r.axes, k.tokens, c.device, positions, stride) || !current_stream(stream, &c.device)) return false;
+    Py_BEGIN_ALLOW_THREADS
+    status = apbv_cache_append(&c.view, to_int(q.heads), to_int(c.heads), to_int(c.d), r.rotation, q.view, k.view, v.view, positions, stride, slots, q_out, stream);
+    Py_END_ALLOW_THREADS
+    return true;
+  });
+}
+
+// ---- requests that share prefixes (apbv_shared.h)
+
+// cache_shared_attention(q, cache, prefix_table, prefix_lengths, block_table, lengths, scale, group_starts, q_starts, max_q, causal, out,
+// lse_out, workspace); group_starts, q_starts and max_q may be None
+PyObject* cache_shared_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (count != 14) return not_taken();
+  return guarded([&](int& status) {
+    Cache c;
+    Tensor q;
+    float scale;
+    int64_t n = -1, groups = -1, max_q = 0, stride, blocks, prefix_stride, prefix_blocks, ws_bytes;
+    int32_t *table, *lengths, *prefix_table, *prefix_lengths, *members = nullptr, *starts = nullptr;
+    void *out, *lse, *ws, *stream;
+    if (!view_of(a[0], q, 3) || !cache_of(a[1], c) || q.device != c.device || q.d != c.d) return false;
+    if (!ints(a[3], groups, c.device, prefix_lengths) || groups < 1 || !ints(a[5], n, c.device, lengths) || n < 1) return false;
+    if (!block_table(a[2], groups, c.device, prefix_table, prefix_stride, prefix_blocks) || !block_table(a[4], n, c.device, table, stride, blocks)) return false;
+    if (!number(a[6], scale) || !PyBool_Check(a[10])) return false;
+    if (a[7] != Py_None) {
+      int64_t entries = groups + 1;
+      if (!ints(a[7], entries, c.device, members)) return false;
+    }
+    if (a[8] != Py_None) {
+      int64_t entries = n + 1;
+      if (!ints(a[8], entries, c.device, starts)) return false;
+    }
+    if (a[9] == Py_None)
+      max_q = starts == nullptr ? q.tokens / n : q.tokens;
+    else if (!whole(a[9], max_q))
+      return false;
+    if (a[11] == Py_None || a[13] == Py_None || !buffer(a[11], at::kBFloat16, q.tokens * q.heads * q.d, c.device, false, out) ||
+        !buffer(a[12], at::kFloat, q.heads * q.tokens, c.device, true, lse) || !buffer(a[13], at::kByte, 0, c.device, false, ws, &ws_bytes) ||
+        !current_stream(stream, &c.device))
+      return false;
+    if (q.tokens == 0) out = nullptr;
+    const int causal = a[10] == Py_True;
+    Py_BEGIN_ALLOW_THREADS
+    status = apbv_cache_shared_attention(&c.view, to_int(groups), to_int(n), to_int(q.heads), to_int(c.heads), to_int(c.d), q.view, prefix_table, prefix_stride,
+                                         prefix_blocks, prefix_lengths, members, table, stride, blocks, lengths, starts, max_q, causal, scale, out,
+                                         static_cast<float*>(lse), ws, (size_t)ws_bytes, stream);
+    Py_END_ALLOW_THREADS
+    return true;
+  });
+}
+
 // use_stream(is_initialized, current_device, raw_stream): the functions that name the current stream
 PyObject* use_stream(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 3) {
@@ -438,7 +570,7 @@ PyObject* use_stream(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define APBV_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {APBV_METHOD(merge_lse), APBV_METHOD(host_attention), APBV_METHOD(query_attention), APBV_METHOD(attention_group),
                          APBV_METHOD(compress_kv), APBV_METHOD(cache_map), APBV_METHOD(cache_store), APBV_METHOD(cache_load), APBV_METHOD(cache_attention),
-                         APBV_METHOD(use_stream), {nullptr, nullptr, 0, nullptr}};
+                         APBV_METHOD(rotate), APBV_METHOD(cache_append), APBV_METHOD(cache_shared_attention), APBV_METHOD(use_stream), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -63,9 +63,18 @@ class ApbvRotation:
         if not (eps >= 0.0 and math.isfinite(eps)):
             raise ValueError("eps: expected a finite number, not negative")
         self.inv_freq, self.q_weight, self.k_weight, self.head_dim = inv_freq, q_weight, k_weight, head_dim
+        self._made_of = (inv_freq, head_dim, axes, bool(adjacent), q_weight, k_weight, eps)
         self.n_axes, self.rot_dim, self.device = max(axes) + 1, 2 * pairs, inv_freq.device
         self._struct = ApbvRotationStruct(inv_freq.data_ptr(), *(w.data_ptr() if w is not None else None for w in (q_weight, k_weight)), eps,
                                           2 * pairs, self.n_axes, int(bool(adjacent)), (ctypes.c_uint8 * 64)(*axes))
+        self._plan = (ctypes.addressof(self._struct), self.n_axes, head_dim, inv_freq.get_device())      # for the native marshalling
+
+    def __reduce__(self):                                             # (a copy has an apbv_rotation of its own)
+        return _rotation_of, self._made_of
+
+
+def _rotation_of(inv_freq, head_dim, axis, adjacent, q_weight, k_weight, eps) -> ApbvRotation:
+    return ApbvRotation(inv_freq, head_dim, axis=axis, adjacent=adjacent, q_weight=q_weight, k_weight=k_weight, eps=eps)
 
 
 def _check_rotation(r: ApbvRotation, d: int, device: torch.device) -> None:
@@ -96,6 +105,12 @@ def apbv_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions:
     ``[tokens]`` or ``[axes, tokens]`` int32; see apbv_rotate in include/apbv_positions.h.  Returns ``(q_out, k_out)``, dense; an output
     may be its input, where that is dense."""
     lib = load_library()
+    if stream is None and type(rotation) is ApbvRotation:
+        st = binding._native.rotate(q, k, positions, rotation._plan, q_out, k_out)
+        if st is not None:
+            if st != 0:
+                raise ApbvError(st, "apbv_rotate")
+            return q_out if q is not None else None, k_out if k is not None else None
     if q is None and k is None:
         raise ValueError("q and k: one of them is needed")
     one = k if q is None else q
@@ -134,6 +149,12 @@ def apbv_cache_append(cache: ApbvCache, q: Optional[torch.Tensor], k: torch.Tens
     """A step's queries turned into ``q_out``, its keys (turned) and values written into the cache at ``slots [tokens]``; see
     apbv_cache_append in include/apbv_positions.h.  Returns ``q_out`` (None without ``q``)."""
     lib = load_library()
+    if stream is None and type(cache) is ApbvCache and type(rotation) is ApbvRotation:
+        st = binding._native.cache_append(cache, q, k, v, slots, positions, rotation._plan, q_out)
+        if st is not None:
+            if st != 0:
+                raise ApbvError(st, "apbv_cache_append")
+            return q_out if q is not None else None
     dev = _rows_device(k, "k", stream)
     view, heads, d = _cache_view(cache, dev)
     n = k.shape[0]

@@ -34,6 +34,13 @@ def apbv_cache_shared_attention(q: torch.Tensor, cache: ApbvCache, prefix_table:
     prefixes, ``group_starts [groups + 1]`` the first request of each group (without it all groups have equally many); the others are
     those of ``apbv_cache_attention``.  Returns ``out [rows, Hq, d]`` bf16 (and ``lse [Hq, rows]`` fp32)."""
     lib = load_library()
+    if stream is None and type(cache) is ApbvCache and out is not None and workspace is not None and not (return_lse and lse_out is None):
+        st = binding._native.cache_shared_attention(q, cache, prefix_table, prefix_lengths, block_table, lengths, softmax_scale, group_starts, q_starts,
+                                                    max_q, causal, out, lse_out, workspace)
+        if st is not None:
+            if st != 0:
+                raise ApbvError(st, "apbv_cache_shared_attention")
+            return (out, lse_out) if return_lse else out
     dev = _rows_device(q, "q", stream)
     view, heads, d = _cache_view(cache, dev)
     if q.dim() != 3 or q.shape[2] != d:
