@@ -52,7 +52,7 @@ apbv_status apbv_rotate(int n_q_heads, int n_kv_heads, int head_dim, const apbv_
  * Keys are formed in float64 and rounded once, to the codes of the cache (a key that apbv_rotate has rounded to bf16 and
  * apbv_cache_store then stores may be held one code away); a NaN is stored as zero, what lies beyond the largest finite bf16 as that.
  * Queries may be left out (0 tokens: keys and values alone).
- * Supported: as apbv_rotate and apbv_cache_store.
+ * Supported: as apbv_rotate and apbv_cache_store; tokens * n_kv_heads up to 2^26.
  */
 apbv_status apbv_cache_append(const apbv_cache* cache, int n_q_heads, int n_kv_heads, int head_dim, const apbv_rotation* rotation,
                               apbv_tensor q, apbv_tensor k, apbv_tensor v, const int32_t* positions, int64_t position_stride,

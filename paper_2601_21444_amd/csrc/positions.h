@@ -12,7 +12,7 @@ struct Rotation {
   int64_t position_stride;
   double eps;
   int rot, adjacent;
-  uint8_t axis[kMaxPairs];
+  uint64_t axis[2];        // two bits a pair, 32 pairs each
 };
 inline Rotation to_rotation(const apbv_rotation& r, const int32_t* positions, int64_t stride) {
   Rotation x;
@@ -24,7 +24,8 @@ inline Rotation to_rotation(const apbv_rotation& r, const int32_t* positions, in
   x.eps = r.eps;
   x.rot = r.rot_dim;
   x.adjacent = r.adjacent;
-  for (int i = 0; i < kMaxPairs; ++i) x.axis[i] = i < r.rot_dim / 2 ? r.axis[i] : 0;
+  x.axis[0] = x.axis[1] = 0;
+  for (int i = 0; i < r.rot_dim / 2; ++i) x.axis[i / 32] |= (uint64_t)r.axis[i] << (2 * (i % 32));
   return x;
 }
 
@@ -42,7 +43,8 @@ struct AppendParams {
   CacheView cache;
   View k, v;
   const int32_t* slots;
-  int hkv, query_groups;   // workgroups of the queries, in front of those of keys and values
+  int hkv, row_groups;     // workgroups of keys and values, in front of those of the queries
+  int tile_tokens, tile_heads, head_tiles;      // append_plan
 };
 apbv_status launch_rotate(TurnParams& p, int head_dim, hipStream_t stream);
 apbv_status launch_cache_append(AppendParams& p, int head_dim, hipStream_t stream);

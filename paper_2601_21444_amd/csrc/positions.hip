@@ -51,8 +51,24 @@ __device__ __forceinline__ Turn turn_of(int position, float inv_freq) {
   y.s = quarter >= 2 ? -y.s : y.s;
   return y;
 }
-__device__ __forceinline__ Turn turn_at(const Rotation& r, int64_t token, int pair) {
-  return turn_of(r.positions[r.axis[pair] * r.position_stride + token], r.inv_freq[pair]);
+// f(token, pair, its turn) for the pairs of `tokens` tokens from t0 on, dealt to 256 threads.
+template <int D, typename F>
+__device__ __forceinline__ void for_turns(const Rotation& r, int64_t t0, int tokens, F&& f) {
+  constexpr int kPairs = D / 2;
+  const int pair = threadIdx.x % kPairs;
+  if (2 * pair >= r.rot) return;
+  const int axis = (int)((pair < 32 ? r.axis[0] : r.axis[1]) >> (2 * (pair % 32))) & 3;
+  const int32_t* positions = r.positions + axis * r.position_stride + t0;
+  const float inv_freq = r.inv_freq[pair];
+  for (int t = threadIdx.x / kPairs; t < tokens; t += 256 / kPairs) f(t, pair, turn_of(positions[t], inv_freq));
+}
+// 1 / sqrt(x): the instruction's 24 bits, doubled by a Newton step for each that is asked for.
+template <int kSteps>
+__device__ __forceinline__ double inv_sqrt(double x) {
+  double y = __builtin_amdgcn_rsq(x);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) y = __builtin_fma(y * 0.5, __builtin_fma(-x * y, y, 1.0), y);
+  return y;
 }
 
 __device__ __forceinline__ float low(uint32_t x) { return __uint_as_float(x << 16); }
@@ -80,7 +96,7 @@ __device__ __forceinline__ double group_sum(double x) {
 // The cosines and sines of a workgroup's tokens: float32 [token][2][pair] of rows that go to bf16, Turn [token][pair] of keys for the cache.
 extern __shared__ __attribute__((aligned(16))) float angles[];
 constexpr size_t turn_lds_bytes(const TurnParams& p) { return (size_t)p.tile_tokens * p.rot.rot * sizeof(float); }
-constexpr size_t append_lds_bytes(int d, int rot) { return (size_t)(2048 / d) * (rot / 2) * sizeof(Turn); }
+constexpr size_t append_lds_bytes(const AppendParams& p) { return (size_t)p.tile_tokens * (p.turn.rot.rot / 2) * sizeof(Turn); }
 
 // The rows of token tile and head tile `group`, kRows a thread.
 template <int D, int kRows>
@@ -97,7 +113,8 @@ __device__ __forceinline__ void turn_rows_of(const TurnParams& p, uint32_t group
 
   int token[kRows], head[kRows];
   bool live[kRows];
-  u32x4 x[kRows][2];
+  u32x4 x[kRows][2], wq[2], wk[2];
+  const bool q_normed = p.rot.q_weight != nullptr, k_normed = p.rot.k_weight != nullptr;
   {
     const int row = threadIdx.x / L;
     int t = row / p.tile_heads, h = row - t * p.tile_heads;
@@ -120,16 +137,15 @@ __device__ __forceinline__ void turn_rows_of(const TurnParams& p, uint32_t group
       h += step_h;
       if (h >= p.tile_heads) h -= p.tile_heads, ++t;
     }
+    if (q_normed) wq[0] = *reinterpret_cast<const u32x4*>(p.rot.q_weight + e0), wq[1] = *reinterpret_cast<const u32x4*>(p.rot.q_weight + e1);
+    if (k_normed) wk[0] = *reinterpret_cast<const u32x4*>(p.rot.k_weight + e0), wk[1] = *reinterpret_cast<const u32x4*>(p.rot.k_weight + e1);
   }
 
   // cosines and sines [token][2][half]
-  const int n = (int)(p.tokens - t0 < p.tile_tokens ? p.tokens - t0 : p.tile_tokens) * half;
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const int t = i / half, pair = i - t * half;
-    const Turn y = turn_at(p.rot, t0 + t, pair);
+  for_turns<D>(p.rot, t0, (int)(p.tokens - t0 < p.tile_tokens ? p.tokens - t0 : p.tile_tokens), [&](int t, int pair, const Turn& y) {
     lds[t * 2 * half + pair] = (float)y.c;
     lds[(t * 2 + 1) * half + pair] = (float)y.s;
-  }
+  });
   __syncthreads();
 
 #pragma unroll
@@ -143,23 +159,22 @@ __device__ __forceinline__ void turn_rows_of(const TurnParams& p, uint32_t group
         y[s][2 * i] = low(x[u][s][i]);
         y[s][2 * i + 1] = high(x[u][s][i]);
       }
-    const bf16_t* weight = is_q ? p.rot.q_weight : p.rot.k_weight;
-    if (weight != nullptr) {
-      const u32x4 w0 = *reinterpret_cast<const u32x4*>(weight + e0), w1 = *reinterpret_cast<const u32x4*>(weight + e1);
+    if (is_q ? q_normed : k_normed) {
       double sum = 0.0;
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = __builtin_fma((double)y[s][i], (double)y[s][i], sum);
       sum = group_sum<L>(sum);
-      const float scale = (float)(1.0 / __builtin_sqrt(sum / D + p.rot.eps));
+      const float scale = (float)inv_sqrt<1>(__builtin_fma(sum, 1.0 / D, p.rot.eps));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        y[0][2 * i] *= scale * low(w0[i]);
-        y[0][2 * i + 1] *= scale * high(w0[i]);
-        y[1][2 * i] *= scale * low(w1[i]);
-        y[1][2 * i + 1] *= scale * high(w1[i]);
-      }
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t w = is_q ? wq[s][i] : wk[s][i];
+          y[s][2 * i] *= scale * low(w);
+          y[s][2 * i + 1] *= scale * high(w);
+        }
     }
     if (turned) {
       const float* table = lds + (live[u] ? token[u] : 0) * 2 * half;
@@ -246,30 +261,33 @@ __device__ __forceinline__ uint32_t encode64(const double (&x)[8], uint32_t& sca
   return c;
 }
 
-// One head of 256 / (D / 8) consecutive tokens; the neighbour takes the next head of them.
+// 256 / (D / 8) rows: a few heads of consecutive tokens, which share the angles; the tokens of a head follow one another in a page, and
+// their codes are written in whole lines.
 template <int D>
 __device__ __forceinline__ void append_rows(const AppendParams& p, uint32_t group, Turn* lds) {
-  constexpr int kPieces = D / 8, kTokens = 256 / kPieces;
+  constexpr int kPieces = D / 8;
   const Rotation& r = p.turn.rot;
-  const int64_t tokens = p.turn.tokens, t0 = (int64_t)(group / (uint32_t)p.hkv) * kTokens;
-  const int head = (int)(group % (uint32_t)p.hkv), piece = threadIdx.x % kPieces, t = threadIdx.x / kPieces, half = r.rot >> 1;
-  const bool live = t0 + t < tokens;
-  const int64_t token = live ? t0 + t : tokens - 1;
+  const uint32_t tt = group / (uint32_t)p.head_tiles;
+  const int64_t tokens = p.turn.tokens, t0 = (int64_t)tt * p.tile_tokens;
+  const int row = threadIdx.x / kPieces, piece = threadIdx.x % kPieces, half = r.rot >> 1;
+  const int h = row / p.tile_tokens, t = row - h * p.tile_tokens;
+  const int h0 = (int)(group - tt * (uint32_t)p.head_tiles) * p.tile_heads;
+  const bool live = h < p.tile_heads && h0 + h < p.hkv && t0 + t < tokens;
+  const int head = live ? h0 + h : h0;
+  const int64_t token = live ? t0 + t : t0;
   const int e0 = 8 * piece;
   const bool turned = e0 < r.rot, upper = !r.adjacent && e0 >= half;
   const int slot = p.slots[token];
-  const bf16_t* row = p.k.ptr + token * p.k.st + (int64_t)head * p.k.sh;
-  const u32x4 k = *reinterpret_cast<const u32x4*>(row + e0);
+  const bf16_t* from = p.k.ptr + token * p.k.st + (int64_t)head * p.k.sh;
+  const u32x4 k = *reinterpret_cast<const u32x4*>(from + e0);
   const int with = !turned || r.adjacent ? e0 : (upper ? e0 - half : e0 + half);
-  const u32x4 k_with = *reinterpret_cast<const u32x4*>(row + with);      // the elements that these turn with
+  const u32x4 k_with = *reinterpret_cast<const u32x4*>(from + with);      // the elements that these turn with
   const u32x4 v = *reinterpret_cast<const u32x4*>(p.v.ptr + token * p.v.st + (int64_t)head * p.v.sh + e0);
+  u32x4 w, w_with;
+  if (r.k_weight != nullptr) w = *reinterpret_cast<const u32x4*>(r.k_weight + e0), w_with = *reinterpret_cast<const u32x4*>(r.k_weight + with);
 
   // [token][pair]
-  const int n = (int)(tokens - t0 < kTokens ? tokens - t0 : kTokens) * half;
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const int at = i / half;
-    lds[i] = turn_at(r, t0 + at, i - at * half);
-  }
+  for_turns<D>(r, t0, (int)(tokens - t0 < p.tile_tokens ? tokens - t0 : p.tile_tokens), [&](int at, int pair, const Turn& y) { lds[at * half + pair] = y; });
   __syncthreads();
 
   double x[8], y[8];
@@ -279,12 +297,11 @@ __device__ __forceinline__ void append_rows(const AppendParams& p, uint32_t grou
     y[2 * i] = low(k_with[i]), y[2 * i + 1] = high(k_with[i]);
   }
   if (r.k_weight != nullptr) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(r.k_weight + e0), w_with = *reinterpret_cast<const u32x4*>(r.k_weight + with);
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum = __builtin_fma(x[i], x[i], sum);
     sum = group_sum<kPieces>(sum);
-    const double scale = 1.0 / __builtin_sqrt(sum / D + r.eps);
+    const double scale = inv_sqrt<2>(__builtin_fma(sum, 1.0 / D, r.eps));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       x[2 * i] *= scale * low(w[i]), x[2 * i + 1] *= scale * high(w[i]);
@@ -326,10 +343,10 @@ __device__ __forceinline__ void append_rows(const AppendParams& p, uint32_t grou
 
 template <int D, int kRows>
 __global__ __launch_bounds__(256) void cache_append_kernel(const AppendParams p) {
-  if (blockIdx.x < (uint32_t)p.query_groups)
-    turn_rows_of<D, kRows>(p.turn, blockIdx.x, angles);
+  if (blockIdx.x < (uint32_t)p.row_groups)
+    append_rows<D>(p, blockIdx.x, reinterpret_cast<Turn*>(angles));
   else
-    append_rows<D>(p, blockIdx.x - (uint32_t)p.query_groups, reinterpret_cast<Turn*>(angles));
+    turn_rows_of<D, kRows>(p.turn, blockIdx.x - (uint32_t)p.row_groups, angles);
 }
 
 // Fills in how the rows are dealt; the number of workgroups.
@@ -353,13 +370,17 @@ apbv_status launch_rotate(TurnParams& p, int d, hipStream_t stream) {
 }
 
 apbv_status launch_cache_append(AppendParams& p, int d, hipStream_t stream) {
-  const int64_t rows = p.turn.tokens * p.turn.hq;
-  p.query_groups = p.turn.hq > 0 ? (int)deal_rows(p.turn, rows, d) : 0;
+  const int64_t rows = p.turn.tokens * p.turn.hq, query_groups = p.turn.hq > 0 ? deal_rows(p.turn, rows, d) : 0;
+  const TurnPlan plan = append_plan(p.turn.tokens, p.hkv, d);
+  p.tile_tokens = plan.tokens;
+  p.tile_heads = plan.heads;
+  p.head_tiles = (int)plan.head_tiles;
+  p.row_groups = (int)plan.workgroups();
   auto kernel = turn_rows(rows, d) > 4096 / d ? (d == 128 ? cache_append_kernel<128, 4> : cache_append_kernel<64, 4>)
                                               : (d == 128 ? cache_append_kernel<128, 1> : cache_append_kernel<64, 1>);
-  const size_t of_keys = append_lds_bytes(d, p.turn.rot.rot), of_queries = p.query_groups > 0 ? turn_lds_bytes(p.turn) : 0;
+  const size_t of_keys = append_lds_bytes(p), of_queries = query_groups > 0 ? turn_lds_bytes(p.turn) : 0;
   Launcher launch(stream);
-  launch(kernel, dim3((unsigned)(p.query_groups + cache_row_groups(p.turn.tokens, p.hkv, d))), dim3(256), of_keys > of_queries ? of_keys : of_queries, p);
+  launch(kernel, dim3((unsigned)(p.row_groups + query_groups)), dim3(256), of_keys > of_queries ? of_keys : of_queries, p);
   return launch.status();
 }
 

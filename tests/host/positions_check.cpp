@@ -44,8 +44,26 @@ int main() {
           CHECK(seen == p.tokens * p.heads);
         }
       }
+  for (int d : {64, 128})
+    for (int hkv : {1, 2, 3, 5, 7, 8, 9, 16, 17, 100, 65535})
+      for (int64_t tokens : {1, 2, 15, 16, 17, 1000, 100003}) {
+        const TurnPlan p = append_plan(tokens, hkv, d);
+        CHECK(p.tokens >= 2 && p.heads >= 1 && p.tokens * p.heads <= 2048 / d && p.tokens * p.heads > 2048 / d - p.heads);
+        CHECK(p.token_tiles * p.tokens >= tokens && (p.token_tiles - 1) * p.tokens < tokens && p.head_tiles * p.heads >= hkv && (p.head_tiles - 1) * p.heads < hkv);
+        CHECK((size_t)p.tokens * (d / 2) * 16 <= 65536);
+      }
   CHECK(turn_plan((int64_t)1 << 24, 31, turn_rows((int64_t)31 << 24, 128)).workgroups() <= kMaxGroups);
   CHECK(turn_plan(((int64_t)1 << 29) / 65 - 1, 65, turn_rows(((int64_t)1 << 29) - 65, 128)).workgroups() <= kMaxGroups);
+  // the most workgroups that an append may take: as many keys as are supported, and queries up to the limit of both
+  for (int d : {64, 128})
+    for (int hkv : {1, 2, 3, 5, 7, 8, 9, 15, 16, 17, 63, 64, 65, 1000, 65535})
+      for (int64_t tokens : {((int64_t)1 << 26) / hkv, ((int64_t)1 << 26) / hkv / 3, ((int64_t)1 << 24)}) {
+        if (tokens > kMaxTokens || tokens * hkv > (int64_t)1 << 26) continue;
+        for (int hq : {1, 2, 31, 33, 64, 65, 127, 128, 129, 65535}) {
+          if (tokens * (hq + hkv) >= (int64_t)1 << 29) continue;
+          CHECK(append_plan(tokens, hkv, d).workgroups() + turn_plan(tokens, hq, turn_rows(tokens * hq, d)).workgroups() <= kMaxGroups);
+        }
+      }
   apbv_rotation r = {};
   CHECK(check_rotation(nullptr, 128) == APBV_ERR_NULL);
   r.rot_dim = 128;
