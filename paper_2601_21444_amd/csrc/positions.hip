@@ -209,7 +209,14 @@ __device__ __forceinline__ void turn_rows_of(const TurnParams& p, uint32_t group
         u32x4 o;
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = to_pair(y[s][2 * i], y[s][2 * i + 1]);
-        *reinterpret_cast<u32x4*>(to + (s ? e1 : e0)) = o;
+        u32x4* dst = reinterpret_cast<u32x4*>(to + (s ? e1 : e0));
+        // (of many rows past the caches' write-back, which leaves the rows that are read their room: 16384 tokens of 16 + 2 heads of 128
+        // 35.1 -> 25.2 us a call, 32768 of 28 + 4 105.2 -> 96.6; reads past the caches, too: 28.6 and 94.3; with apbv_compress_kv, which
+        // reads the keys, behind it 52.3 -> 44.2)
+        if constexpr (kRows > 1)
+          __builtin_nontemporal_store(o, dst);
+        else
+          *dst = o;
       }
     }
   }
