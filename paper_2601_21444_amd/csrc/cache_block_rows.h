@@ -24,8 +24,8 @@ struct BlockRowsLds {
 };
 
 // kLse, kKept, `block` of `workgroups`: as in cache_few_rows.h.
-template <int D, bool kLse, bool kKept = false, bool kGroups = false>
-__device__ __forceinline__ void attend_block_rows(const CacheAttnParams& p, BlockRowsLds<D>& shared, uint32_t block, uint32_t workgroups) {
+template <int D, bool kLse, bool kKept = false, bool kGroups = false, typename P>
+__device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& shared, uint32_t block, uint32_t workgroups) {
   using T = Tile<D, 1, true>;
   constexpr int W = kCacheWaves, R = kCacheBlockRows;
   static_assert(R == 32 * W, "a wave owns 32 rows");
@@ -36,7 +36,8 @@ __device__ __forceinline__ void attend_block_rows(const CacheAttnParams& p, Bloc
   auto& v_lds = shared.v;
   auto& gone_lds = shared.gone;
 
-  const int lane = threadIdx.x & 63;
+  int lane = threadIdx.x & 63;
+  if constexpr (kKept) asm volatile("" : "+v"(lane));       // (what follows from it is not kept in registers across the work of the other axis)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hh = lane >> 5;
   Axis<R, kGroups> axis(p);

@@ -26,8 +26,8 @@ struct FewRowsLds {
 // kLse: the log-sum-exp is wanted, and the weights are added up before they are rounded, too: their rounded sum, which the
 // output is divided by, would leave it with errors of 2^-9 over the square root of the number of keys.
 // `block` of `workgroups`: which share.
-template <int D, int NQ, bool kOnePage, bool kLse, Form kForm, bool kGroups = false>
-__device__ __forceinline__ void attend_few_rows(const CacheAttnParams& p, FewRowsLds<D, NQ, kForm == Form::kWhole>& shared, uint32_t block,
+template <int D, int NQ, bool kOnePage, bool kLse, Form kForm, bool kGroups = false, typename P>
+__device__ __forceinline__ void attend_few_rows(const P& p, FewRowsLds<D, NQ, kForm == Form::kWhole>& shared, uint32_t block,
                                                 uint32_t workgroups) {
   using T = Tile<D, 1>;
   constexpr int W = kCacheWaves, R = 16 * NQ;
@@ -38,9 +38,10 @@ __device__ __forceinline__ void attend_few_rows(const CacheAttnParams& p, FewRow
   auto& kept = shared.kept;
   auto& place = shared.place;
 
-  const int lane = threadIdx.x & 63;
+  int lane = threadIdx.x & 63;
+  if constexpr (kKept) asm volatile("" : "+v"(lane));       // (what follows from it is not kept in registers across the work of the other axis)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int li = lane & 15, lg = lane >> 4;
+  const int li = lane & 15, lg = lane >> 4, thread = kKept ? 64 * wave + lane : (int)threadIdx.x;
   int keeps = 0, wg = 0;
 
   // per-lane LDS offsets: V rows as written, and as the A operand of O^T (query_attention.hip)
@@ -333,7 +334,7 @@ __device__ __forceinline__ void attend_few_rows(const CacheAttnParams& p, FewRow
       const int slot = chain > 0 ? 1 : 0;                    // a part that begins a row tile, or one that goes on with it
       float* part = p.parts + ((int64_t)wg * 2 + slot) * (R * D);
       float* part_stat = part_stats(p, slot, R, D) + wg;
-      for (int x = threadIdx.x; x < R * (D / 8); x += 64 * W) {
+      for (int x = thread; x < R * (D / 8); x += 64 * W) {
         const int row = x / (D / 8), c = x % (D / 8);
         if (r0 + row >= rows) break;
         // (all waves' statistics, then all waves' rows, are read at once, those of others than the chain's left out)
@@ -402,7 +403,7 @@ __device__ __forceinline__ void attend_few_rows(const CacheAttnParams& p, FewRow
       if (t0 < t1) piece(rq, b, head, rt, t0, t1);
       put_together();
       if (rq.tiles == 0)
-        for (int x = threadIdx.x; x < R * (D / 8); x += 64 * W) {
+        for (int x = thread; x < R * (D / 8); x += 64 * W) {
           const int row = rt * R + x / (D / 8), c = x % (D / 8);
           if (row >= rq.rows) break;
           const int i = query_of(p, row), h = head * p.group + row - i * p.group;

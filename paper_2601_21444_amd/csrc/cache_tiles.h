@@ -10,9 +10,12 @@ namespace {
 #define APBV_CONST(T) const __attribute__((address_space(4))) T*     // read through the scalar cache
 __device__ __forceinline__ int scalar_load(const int32_t* p, int64_t i) { return ((APBV_CONST(int32_t))p)[i]; }
 
+// Parameters: P is CacheAttnParams, or that type in the address space of a kernel's arguments, read where they are used.
+
 // The query that a row (query x head of the group, below 2^30) is of.  (row + 1/2) / group is no nearer to a whole number than 1 /
 // (2 group), the double's error is below 2^-20: three instructions where the division of integers has twenty.
-__device__ __forceinline__ int query_of(const CacheAttnParams& p, int row) { return (int)(((double)row + 0.5) * p.per_group); }
+template <typename P>
+__device__ __forceinline__ int query_of(const P& p, int row) { return (int)(((double)row + 0.5) * p.per_group); }
 
 struct Request {
   int first, rows, len;      // first query, rows (query x head of the group), keys
@@ -20,7 +23,8 @@ struct Request {
 };
 
 __device__ __forceinline__ int clip(int x, int hi) { return x < 0 ? 0 : (x > hi ? hi : x); }
-__device__ __forceinline__ Request request_of(const CacheAttnParams& p, int first, int past, int len) {
+template <typename P>
+__device__ __forceinline__ Request request_of(const P& p, int first, int past, int len) {
   Request r;
   r.first = clip(first, p.n_rows);
   past = clip(past, p.n_rows);
@@ -52,12 +56,13 @@ __device__ __forceinline__ float log_sum(float m, float l) {
   return (float)(x * 0.69314718055994530942);
 }
 // Statistics of the parts of a workgroup that begin a row tile (slot 1) or go on with one (slot 0): maxima, sums, exact sums.
-__device__ __forceinline__ float* part_stats(const CacheAttnParams& p, int slot, int R, int D) {
+template <typename P>
+__device__ __forceinline__ float* part_stats(const P& p, int slot, int R, int D) {
   return p.parts + (int64_t)p.workgroups * 2 * (R * D) + (int64_t)slot * (3 * R) * p.workgroups;
 }
 // ... and of a row that is kept whole, the at-th of [n_rows, Hq].
-template <int D, bool kLse>
-__device__ __forceinline__ void keep_stats(const CacheAttnParams& p, int64_t at, float m, float l, float exact) {
+template <int D, bool kLse, typename P>
+__device__ __forceinline__ void keep_stats(const P& p, int64_t at, float m, float l, float exact) {
   const int64_t n = (int64_t)p.n_rows * p.hq;
   float* stat = p.kept + n * D + at;
   stat[0] = m;
@@ -79,19 +84,23 @@ struct Axis {
   uint32_t group_past;       // ... and where it ends
 
   __device__ __forceinline__ static uint32_t top(uint32_t x) { return x < 0x7fff0000u ? x : 0x7fff0000u; }
-  __device__ __forceinline__ static uint32_t tiles(const CacheAttnParams& p, const Request& r) {
+  template <typename P>
+  __device__ __forceinline__ static uint32_t tiles(const P& p, const Request& r) {
     return (uint32_t)((r.rows + R - 1) / R * p.hkv) * (uint32_t)r.tiles;
   }
-  __device__ __forceinline__ static int first_row(const CacheAttnParams& p, int b) {
+  template <typename P>
+  __device__ __forceinline__ static int first_row(const P& p, int b) {
     if constexpr (kGroups)
       if (p.members_each > 0) b = p.members ? clip(p.members[b], p.n_members) : b * p.members_each;      // a group's first request
     return p.starts ? p.starts[b] : b * p.each;
   }
-  __device__ __forceinline__ static Request load(const CacheAttnParams& p, int b) {
+  template <typename P>
+  __device__ __forceinline__ static Request load(const P& p, int b) {
     const int first = first_row(p, b), past_row = first_row(p, b + 1);
     return request_of(p, first, past_row, p.lengths[b]);
   }
-  __device__ __forceinline__ void window(const CacheAttnParams& p, int from, uint32_t begin) {
+  template <typename P>
+  __device__ __forceinline__ void window(const P& p, int from, uint32_t begin) {
     base = from;
     base_begin = begin;
     mine = Request{0x7fffffff, 0, 0, 0};
@@ -99,7 +108,8 @@ struct Axis {
     if (b < p.n_requests) mine = load(p, b);
     past = add_sat(begin, wave_scan(tiles(p, mine)));
   }
-  __device__ __forceinline__ Axis(const CacheAttnParams& p) {
+  template <typename P>
+  __device__ __forceinline__ Axis(const P& p) {
     if (p.n_requests <= 64) {
       window(p, 0, 0);
       total = top(__builtin_amdgcn_readlane(past, 63));
@@ -124,7 +134,8 @@ struct Axis {
   }
   // Of the rows alone, for find_row: whoever takes a request's first tile leaves word of where it begins.
   struct RowsOnly {};
-  __device__ __forceinline__ Axis(const CacheAttnParams& p, RowsOnly) {
+  template <typename P>
+  __device__ __forceinline__ Axis(const P& p, RowsOnly) {
     if (p.n_requests <= 64) {
       window(p, 0, 0);
       total = top(__builtin_amdgcn_readlane(past, 63));
@@ -136,20 +147,22 @@ struct Axis {
     if (b < p.n_requests) group_first = clip(first_row(p, b), p.n_rows);
     group_past = 0;
   }
-  template <bool kAlways = false>
-  __device__ __forceinline__ void leave_word(const CacheAttnParams& p, int b, uint32_t begin, uint32_t share) const {
+  template <bool kAlways = false, typename P>
+  __device__ __forceinline__ void leave_word(const P& p, int b, uint32_t begin, uint32_t share) const {
     if ((kAlways || p.n_requests > 64) && (threadIdx.x & 63) == 0) {
       p.begins[1 + b] = begin;
       if (begin == 0) p.begins[0] = share;
     }
   }
-  __device__ __forceinline__ void group_window(const CacheAttnParams& p, int group) {
+  template <typename P>
+  __device__ __forceinline__ void group_window(const P& p, int group) {
     window(p, group * per, group > 0 ? __builtin_amdgcn_readlane(group_past, group - 1) : 0);
   }
   __device__ __forceinline__ uint32_t begin_of(int b) const {                   // b of the window
     return b > base ? __builtin_amdgcn_readlane(past, b - base - 1) : base_begin;
   }
-  __device__ __forceinline__ Request at(const CacheAttnParams& p, int b) {     // b uniform
+  template <typename P>
+  __device__ __forceinline__ Request at(const P& p, int b) {     // b uniform
     if ((unsigned)(b - base) >= 64u) window(p, b, 0);      // (a walk that leaves the window knows where it is)
     Request r;
     r.first = __builtin_amdgcn_readlane(mine.first, b - base);
@@ -159,10 +172,12 @@ struct Axis {
     return r;
   }
   // Length of a workgroup's share, of as many as there are.
-  __device__ __forceinline__ uint32_t share(const CacheAttnParams& p, uint32_t workgroups) const {
+  template <typename P>
+  __device__ __forceinline__ uint32_t share(const P& p, uint32_t workgroups) const {
     return cache_share(total, workgroups, (uint32_t)p.short_tiles, (uint32_t)p.least_tiles, (uint32_t)p.share_step);
   }
-  __device__ __forceinline__ uint32_t share(const CacheAttnParams& p) const { return share(p, (uint32_t)p.workgroups); }
+  template <typename P>
+  __device__ __forceinline__ uint32_t share(const P& p) const { return share(p, (uint32_t)p.workgroups); }
   // The share of this workgroup, or -1: consecutive shares on one XCD (row tiles of a head read the same keys), which a launch
   // gives its workgroups in turn.
   __device__ __forceinline__ int my_share(uint32_t share, uint32_t block) const {
@@ -171,12 +186,14 @@ struct Axis {
     return x < per_xcd && wg < n ? wg : -1;
   }
   // The request that holds tile `pos` < total.
-  __device__ __forceinline__ int find(const CacheAttnParams& p, uint32_t pos) {
+  template <typename P>
+  __device__ __forceinline__ int find(const P& p, uint32_t pos) {
     if (p.n_requests > 64) group_window(p, __builtin_ctzll(__builtin_amdgcn_ballot_w64(group_past > pos)));
     return base + __builtin_ctzll(__builtin_amdgcn_ballot_w64(past > pos));
   }
   // The last request that begins at or before this query row (the first one if there is none).
-  __device__ __forceinline__ int find_row(const CacheAttnParams& p, int row) {
+  template <typename P>
+  __device__ __forceinline__ int find_row(const P& p, int row) {
     if (p.n_requests > 64) {
       const uint64_t before = __builtin_amdgcn_ballot_w64(group_first <= row);
       group_window(p, before ? 63 - __builtin_clzll(before) : 0);
@@ -224,7 +241,8 @@ template <int D, bool kOnePage>
 struct Blocks {
   int64_t codes, scales;
   int absent;                // the page is out of range, or no key of the request lies in it
-  __device__ __forceinline__ void find(const CacheAttnParams& p, const int32_t* table_row, int head, int len, int tile) {
+  template <typename P>
+  __device__ __forceinline__ void find(const P& p, const int32_t* table_row, int head, int len, int tile) {
     const int token = tile * kCacheKeyTile, at = token < len ? token : len - 1;      // (a table entry that the request has)
     const int page = scalar_load(table_row, at >> p.cache.page_log2);
     const bool there = token < len && (unsigned)page < (unsigned)p.cache.n_pages;
@@ -249,11 +267,13 @@ struct Blocks<D, false> {
   int64_t codes, scales;
   int absent;                // bit i: of block i, uniform
   __device__ __forceinline__ static int token_of(int tile) { return tile * kCacheKeyTile + 16 * (int)(threadIdx.x & 3); }
-  __device__ __forceinline__ static int look_up(const CacheAttnParams& p, const int32_t* table_row, int len, int tile) {
+  template <typename P>
+  __device__ __forceinline__ static int look_up(const P& p, const int32_t* table_row, int len, int tile) {
     const int token = token_of(tile);
     return table_row[(token < len ? token : len - 1) >> p.cache.page_log2];
   }
-  __device__ __forceinline__ void place(const CacheAttnParams& p, int head, int len, int tile, int page) {
+  template <typename P>
+  __device__ __forceinline__ void place(const P& p, int head, int len, int tile, int page) {
     const int token = token_of(tile);
     const bool there = token < len && (unsigned)page < (unsigned)p.cache.n_pages;
     absent = (int)(~__builtin_amdgcn_ballot_w64(there) & 15);

@@ -2,9 +2,8 @@
 //
 // The rows of a group are one problem over its prefix, as many rows as its requests have together: the prefix is read and converted once
 // for up to 128 of them, and what it costs is matrix instructions, not bytes.  The rows of a request over its own keys are the problem of
-// cache_attention.hip.  Both lie on axes of tiles of their own, cut into equal shares, and run in one launch: as many workgroups
-// as their tiles cost take shares of the one axis and the others of the other, so that what is bound by matrix instructions runs beside
-// what is bound by memory.  A row's parts, of either axis, are left in float32 and joined by a second launch.
+// cache_attention.hip.  Both lie on axes of tiles of their own, cut into equal shares, in one launch.  A row's parts, of either
+// axis, are left in float32 and joined by a second launch.
 #include "cache_block_rows.h"
 #include "cache_few_rows.h"
 #include "shared.h"
@@ -21,131 +20,159 @@ struct LdsOf<D, kCacheBlockRows> {
   typedef BlockRowsLds<D> type;
 };
 
-template <int D, int R, bool kOnePage, bool kLse, bool kGroups>
-__device__ __forceinline__ void attend(const CacheAttnParams& p, typename LdsOf<D, R>::type& lds, uint32_t block, uint32_t workgroups) {
+template <int D, int R, bool kOnePage, bool kLse, bool kGroups, typename P>
+__device__ __forceinline__ void attend(const P& p, typename LdsOf<D, R>::type& lds, uint32_t block, uint32_t workgroups) {
   if constexpr (R == kCacheBlockRows)
     attend_block_rows<D, kLse, true, kGroups>(p, lds, block, workgroups);
   else
     attend_few_rows<D, R / 16, kOnePage, kLse, Form::kKept, kGroups>(p, lds, block, workgroups);
 }
 
-// What a tile of 64 keys costs, R rows.
-constexpr uint64_t tile_cost(int rows) { return rows == kCacheBlockRows ? 3 : 1; }
-
+// Every workgroup has a share of either axis, or of one of them where they are short: those of the prefixes are dealt from the first
+// workgroup on, those of the own keys from the last.  Half of the workgroups begin with the one and half with the other, so that beside
+// a workgroup that is bound by matrix instructions one runs that is bound by memory, and all end together.
 template <int D, int RP, int RO, bool kOnePage, bool kLse>
-__global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_attention_kernel(const SharedParams p) {
+__global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_attention_kernel(const SharedParams) {
   __shared__ union Lds {
     typename LdsOf<D, RP>::type prefix;
     typename LdsOf<D, RO>::type own;
     __device__ Lds() {}
   } lds;
-  const uint32_t workgroups = (uint32_t)p.own.workgroups;
-  const uint64_t prefix_cost = Axis<RP, true>(p.prefix).total * tile_cost(RP), own_cost = Axis<RO>(p.own).total * tile_cost(RO);
-  const uint32_t of_prefix = shared_split(workgroups, prefix_cost, own_cost);
-  if constexpr (RP == RO) {
-    const bool on_prefix = blockIdx.x < of_prefix;         // (one body for both)
-    attend<D, RP, kOnePage, kLse, true>(on_prefix ? p.prefix : p.own, lds.prefix, on_prefix ? blockIdx.x : blockIdx.x - of_prefix,
-                                        on_prefix ? of_prefix : workgroups - of_prefix);
-  } else if (blockIdx.x < of_prefix)
-    attend<D, RP, kOnePage, kLse, true>(p.prefix, lds.prefix, blockIdx.x, of_prefix);
-  else
-    attend<D, RO, kOnePage, kLse, false>(p.own, lds.own, blockIdx.x - of_prefix, workgroups - of_prefix);
+  // (arguments are read from where they lie, when they are needed: there are too many for the scalar registers)
+  typedef APBV_CONST(SharedParams) Arguments;
+  Arguments args = (Arguments)__builtin_amdgcn_kernarg_segment_ptr();
+  const uint32_t workgroups = (uint32_t)args->own.workgroups;
+  bool on_prefix = blockIdx.x < workgroups / 2;
+#pragma unroll 1
+  for (int turn = 0; turn < 2; ++turn, on_prefix = !on_prefix) {
+    if (turn > 0) __syncthreads();                         // LDS is free again
+    asm volatile("" : "+s"(args));
+    const uint32_t block = on_prefix ? blockIdx.x : workgroups - 1 - blockIdx.x;
+    if constexpr (RP == RO)                                // (one body for both)
+      attend<D, RP, kOnePage, kLse, true>(on_prefix ? args->prefix : args->own, lds.prefix, block, workgroups);
+    else if (on_prefix)
+      attend<D, RP, kOnePage, kLse, true>(args->prefix, lds.prefix, block, workgroups);
+    else
+      attend<D, RO, kOnePage, kLse, false>(args->own, lds.own, block, workgroups);
+  }
 }
 
-// Where the parts of a row over one axis lie: workgroups `first` to `last`, each with a part of the row tile, or the row kept whole.
+// Where the parts of a row over one axis lie: of the workgroups `first` to `last`, each of which has a part of the row tile, or the row
+// that one has kept whole.
 struct Parts {
-  int first, last;                 // last < first: none
-  bool whole;
+  int first, count;                // none: 0
+  bool whole, of_axis;             // of_axis: the row is one of a request (or of a group)
   const float *rows, *stat;        // of workgroup 0 in slot 0, or of the row
-  int64_t stat_step, slot_rows, slot_stat;
+  int64_t stat_step;
 };
 template <int D, int R, bool kGroups>
 __device__ __forceinline__ Parts parts_of(const CacheAttnParams& p, int row, int h) {
+  typedef Axis<R, kGroups> A;
+  const int lane = threadIdx.x & 63;
+  int base = 0;
+  if (p.n_requests > 64) {                                 // the last 64th of them that begins at or before the row
+    const int per = (p.n_requests + 63) / 64, b = lane * per;
+    const uint64_t before = __builtin_amdgcn_ballot_w64(b < p.n_requests && clip(A::first_row(p, b), p.n_rows) <= row);
+    base = before ? (63 - __builtin_clzll(before)) * per : 0;
+  }
+  // (a window of requests, and where each begins on the axis, asked for together)
+  const int mine = base + lane;
+  Request rq = {0x7fffffff, 0, 0, 0};
+  uint32_t begin = 0;
+  const uint32_t share = p.begins[0];
+  if (mine < p.n_requests) {
+    begin = p.begins[1 + mine];
+    rq = A::load(p, mine);
+  }
+  const uint64_t before = __builtin_amdgcn_ballot_w64(rq.first <= row);
+  const int at = before ? 63 - __builtin_clzll(before) : 0;
+  const int first_row = __builtin_amdgcn_readlane(rq.first, at), rows = __builtin_amdgcn_readlane(rq.rows, at), tiles = __builtin_amdgcn_readlane(rq.tiles, at);
+  const uint32_t its_begin = __builtin_amdgcn_readlane(begin, at), each = __builtin_amdgcn_readfirstlane(share > 0 ? share : 1);
+  const int i = row - first_row;
   Parts x;
-  x.first = 0;
-  x.last = -1;
-  x.whole = false;
-  Axis<R, kGroups> axis(p, typename Axis<R, kGroups>::RowsOnly{});
-  const int b = axis.find_row(p, row);
-  const Request rq = axis.at(p, b);
-  const int i = row - rq.first;
-  if (i < 0 || i * p.group >= rq.rows || rq.tiles == 0) return x;
-  const uint32_t share = (uint32_t)scalar_load(reinterpret_cast<const int32_t*>(p.begins), 0);
-  const uint32_t begin = (uint32_t)scalar_load(reinterpret_cast<const int32_t*>(p.begins), 1 + b);
-  const int r = i * p.group + h % p.group, rt = r / R, row_tiles = (rq.rows + R - 1) / R;
-  const uint32_t from = begin + (uint32_t)(h / p.group * row_tiles + rt) * (uint32_t)rq.tiles;
+  x.of_axis = i >= 0 && i * p.group < rows;
+  const int r = i * p.group + h % p.group, rt = r / R, row_tiles = (rows + R - 1) / R;
+  const uint32_t from = its_begin + (uint32_t)(h / p.group * row_tiles + rt) * (uint32_t)tiles;
   // (requests that overlap, against the contract, may have left no word: whatever it says, reads stay inside the workspace)
-  const uint32_t each = share > 0 ? share : 1, top = (uint32_t)p.workgroups - 1;
-  const uint32_t first = from / each, last = (from + (uint32_t)rq.tiles - 1) / each;
+  const uint32_t top = (uint32_t)p.workgroups - 1, first = from / each, last = (from + (uint32_t)tiles - 1) / each;
   x.first = (int)(first < top ? first : top);
-  x.last = (int)(last < top ? last : top);
-  x.whole = x.first == x.last;
+  x.count = x.of_axis && tiles > 0 ? (int)(last < top ? last : top) - x.first + 1 : 0;
+  x.whole = x.count == 1;
   if (x.whole) {
-    const int64_t at = (int64_t)row * p.hq + h, n = (int64_t)p.n_rows * p.hq;
-    x.rows = p.kept + at * D;
-    x.stat = p.kept + n * D + at;
+    const int64_t row_at = (int64_t)row * p.hq + h, n = (int64_t)p.n_rows * p.hq;
+    x.rows = p.kept + row_at * D;
+    x.stat = p.kept + n * D + row_at;
     x.stat_step = n;
   } else {
-    x.rows = p.parts + (r % R) * D;
-    x.stat = part_stats(p, 0, R, D) + (int64_t)(r % R) * p.workgroups;
+    x.rows = p.parts + (x.of_axis ? r % R : 0) * D;
+    x.stat = part_stats(p, 0, R, D) + (int64_t)(x.of_axis ? r % R : 0) * p.workgroups;
     x.stat_step = (int64_t)R * p.workgroups;
   }
-  x.slot_rows = R * D;
-  x.slot_stat = (int64_t)(3 * R) * p.workgroups;
   return x;
 }
 
-// A wave per (row, head), four a workgroup: joins the parts of the row over its prefix and over its own keys, as cache_join_kernel
-// those over one.
-template <int D, int RP, int RO>
+// kJoin waves per (row, head): joins the parts of the row over its prefix and over its own keys, one list, as cache_join_kernel
+// those over one axis.
+template <int D, int RP, int RO, int kJoin>
 __global__ __launch_bounds__(256) void shared_join_kernel(const SharedParams p) {
   constexpr int kLanes = D / 4;                            // lanes that hold a row, four elements each
   constexpr int kAtOnce = 64 / kLanes;
-  const int lane = threadIdx.x & 63;
-  const int64_t job = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int kLoads = 8, kChunk = kAtOnce * kLoads;
+  __shared__ float shared_max[kJoin], shared_sum[kJoin], shared_exact[kJoin];
+  __shared__ f32x4 shared_acc[kJoin][kLanes];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t job = kJoin == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
   if (job >= (int64_t)p.own.n_rows * p.own.hq) return;
   const int row = (int)(job / p.own.hq), h = (int)(job % p.own.hq);
-  {                                                        // a row of no request?
-    Axis<RO> axis(p.own, typename Axis<RO>::RowsOnly{});
-    const Request rq = axis.at(p.own, axis.find_row(p.own, row));
-    if (row < rq.first || (row - rq.first) * p.own.group >= rq.rows) return;
-  }
+  const Parts a = parts_of<D, RP, true>(p.prefix, row, h), b = parts_of<D, RO, false>(p.own, row, h);
+  if (!b.of_axis) return;                                  // a row of no request
   const int sub = lane / kLanes, c = lane % kLanes;
   const bool with_lse = p.own.lse != nullptr;
+  // part n of the list: its statistics, and its row
+  auto stat_of = [&](int n, int64_t& step) {
+    const bool own = n >= a.count;
+    const int w = own ? b.first + n - a.count : a.first + n;
+    const bool whole = own ? b.whole : a.whole, begins = n == 0 || n == a.count;
+    const int64_t slot = (int64_t)(3 * (own ? RO : RP)) * p.own.workgroups;
+    step = own ? b.stat_step : a.stat_step;
+    return (own ? b.stat : a.stat) + (whole ? 0 : w + (begins ? slot : 0));
+  };
+  auto row_of = [&](int n) {
+    const bool own = n >= a.count;
+    const int w = own ? b.first + n - a.count : a.first + n;
+    const bool whole = own ? b.whole : a.whole, begins = n == 0 || n == a.count;
+    return (own ? b.rows : a.rows) + (whole ? 0 : (2 * (int64_t)w + (begins ? 1 : 0)) * ((own ? RO : RP) * D));
+  };
+  const int count = a.count + b.count, each = (count + kJoin - 1) / kJoin;
+  const int from_part = kJoin == 1 ? 0 : wave * each, past_part = from_part + each < count ? from_part + each : count;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f, exact = 0.f;
-  auto add = [&](const Parts& x) {
-    constexpr int kLoads = 8, kChunk = kAtOnce * kLoads;
-    for (int base = x.first; base <= x.last; base += kChunk) {
-      const int w = base + lane;
-      const bool mine = lane < kChunk && w <= x.last;
-      const float* s = x.stat + (x.whole ? 0 : w + (w == x.first ? x.slot_stat : 0));
-      const float m_part = mine ? s[0] : -INFINITY, l_part = mine ? s[x.stat_step] : 0.f;
-      const float exact_part = mine && with_lse ? s[2 * x.stat_step] : 0.f;
-      f32x4 y[kLoads];
+  for (int base = from_part; base < past_part; base += kChunk) {
+    const bool mine = lane < kChunk && base + lane < past_part;
+    int64_t step;
+    const float* s = stat_of(mine ? base + lane : base, step);
+    const float m_part = mine ? s[0] : -INFINITY, l_part = mine ? s[step] : 0.f;
+    const float exact_part = mine && with_lse ? s[2 * step] : 0.f;
+    f32x4 x[kLoads];
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        const int v = base + u * kAtOnce + sub;
-        y[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (v <= x.last) y[u] = *reinterpret_cast<const f32x4*>(x.rows + 4 * c + (x.whole ? 0 : (2 * (int64_t)v + (v == x.first ? 1 : 0)) * x.slot_rows));
-      }
-      float top = m_part;
-#pragma unroll
-      for (int d = 1; d < kChunk; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-      top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(fmaxf(top, m))));
-      const float m0 = top > -INFINITY ? top : 0.f;
-      const float old = __builtin_amdgcn_exp2f(m - m0), weight = __builtin_amdgcn_exp2f(m_part - m0);
-      m = top;
-      l = __builtin_fmaf(l, old, weight * l_part);         // (this lane's parts; the lanes are added up below)
-      exact = __builtin_fmaf(exact, old, weight * exact_part);
-      acc *= old;
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u) acc += __shfl(weight, u * kAtOnce + sub) * y[u];
+    for (int u = 0; u < kLoads; ++u) {
+      const int n = base + u * kAtOnce + sub;
+      x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (n < past_part) x[u] = *reinterpret_cast<const f32x4*>(row_of(n) + 4 * c);
     }
-  };
-  const Parts of_prefix = parts_of<D, RP, true>(p.prefix, row, h), of_own = parts_of<D, RO, false>(p.own, row, h);
-  add(of_prefix);
-  add(of_own);
+    float top = m_part;
+#pragma unroll
+    for (int d = 1; d < kChunk; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(fmaxf(top, m))));
+    const float m0 = top > -INFINITY ? top : 0.f;
+    const float old = __builtin_amdgcn_exp2f(m - m0), weight = __builtin_amdgcn_exp2f(m_part - m0);
+    m = top;
+    l = __builtin_fmaf(l, old, weight * l_part);           // (this lane's parts; the lanes are added up below)
+    exact = __builtin_fmaf(exact, old, weight * exact_part);
+    acc *= old;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) acc += __shfl(weight, u * kAtOnce + sub) * x[u];
+  }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
   if (with_lse)
@@ -155,6 +182,25 @@ __global__ __launch_bounds__(256) void shared_join_kernel(const SharedParams p) 
   for (int d = kLanes; d < 64; d *= 2)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], d);
+  if constexpr (kJoin > 1) {
+    if (lane == 0) shared_max[wave] = m, shared_sum[wave] = l, shared_exact[wave] = exact;
+    if (sub == 0) shared_acc[wave][c] = acc;
+    __syncthreads();
+    if (wave != 0) return;
+    m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kJoin; ++w) m = fmaxf(m, shared_max[w]);
+    const float m0 = m > -INFINITY ? m : 0.f;
+    l = exact = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kJoin; ++w) {
+      const float weight = __builtin_amdgcn_exp2f(shared_max[w] - m0);
+      l = __builtin_fmaf(shared_sum[w], weight, l);
+      exact = __builtin_fmaf(shared_exact[w], weight, exact);
+      acc += weight * shared_acc[w][c];
+    }
+  }
   if (sub != 0) return;
   const float inv = l > 0.f ? 1.0f / l : 0.f;
   u32x2 y;
@@ -165,25 +211,28 @@ __global__ __launch_bounds__(256) void shared_join_kernel(const SharedParams p) 
 }
 
 template <int D, int RP, int RO>
-void launch_rows(Launcher& launch, const SharedParams& p) {
+void launch_rows(Launcher& launch, const SharedParams& p, int waves) {
   const bool one_page = (1 << p.own.cache.page_log2) >= kCacheKeyTile, lse = p.own.lse != nullptr;
   auto kernel = one_page ? (lse ? shared_attention_kernel<D, RP, RO, true, true> : shared_attention_kernel<D, RP, RO, true, false>)
                          : (lse ? shared_attention_kernel<D, RP, RO, false, true> : shared_attention_kernel<D, RP, RO, false, false>);
   launch(kernel, dim3((unsigned)p.own.workgroups), dim3(64 * kCacheWaves), 0, p);
   const int64_t rows = (int64_t)p.own.n_rows * p.own.hq;
-  launch(shared_join_kernel<D, RP, RO>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, p);
+  if (waves == 4)
+    launch(shared_join_kernel<D, RP, RO, 4>, dim3((unsigned)rows), dim3(256), 0, p);
+  else
+    launch(shared_join_kernel<D, RP, RO, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, p);
 }
 template <int D>
 apbv_status launch_dim(const SharedParams& p, const SharedPlan& plan, hipStream_t stream) {
   Launcher launch(stream);
   if (plan.prefix.rows == 16)
-    launch_rows<D, 16, 16>(launch, p);
+    launch_rows<D, 16, 16>(launch, p, plan.join_waves);
   else if (plan.prefix.rows == 32)
-    launch_rows<D, 32, 16>(launch, p);
+    launch_rows<D, 32, 16>(launch, p, plan.join_waves);
   else if (plan.own.rows == 16)
-    launch_rows<D, kCacheBlockRows, 16>(launch, p);
+    launch_rows<D, kCacheBlockRows, 16>(launch, p, plan.join_waves);
   else
-    launch_rows<D, kCacheBlockRows, kCacheBlockRows>(launch, p);
+    launch_rows<D, kCacheBlockRows, kCacheBlockRows>(launch, p, plan.join_waves);
   return launch.status();
 }
 

@@ -23,10 +23,11 @@ inline apbv_status validate_shared_attention(const apbv_cache* cache, int n_grou
 }
 
 // How a call is cut: two axes of tiles as in cache_validation.h, one of the groups over their prefixes and one of the requests over
-// their own keys, whose workgroups run side by side.
+// their own keys, of both of which every workgroup takes a share.
 struct SharedPlan {
   CachePlan prefix, own;
-  int workgroups;            // of both axes together
+  int workgroups;
+  int join_waves;            // waves that join the parts of a row: 1 or 4
 };
 inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q) {
   SharedPlan p;
@@ -40,17 +41,11 @@ inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int h
     p.own.row_tiles = (int)((rows + 15) / 16);
   }
   p.prefix.workgroups = p.own.workgroups = p.workgroups;
+  // a row has as many parts over its prefix as workgroups share it, if the groups are alike
+  const int64_t parts = p.workgroups / ((int64_t)n_groups * hkv * p.prefix.row_tiles) + 1;
+  p.join_waves = parts > 8 && n_rows * hq <= 2048 ? 4 : 1;
   return p;
 }
-// Workgroups of the prefixes' axis among all: by what its tiles and the others cost (in multiples of 8, one for each die).
-constexpr uint32_t shared_split(uint32_t workgroups, uint64_t prefix_cost, uint64_t own_cost) {
-  if (own_cost == 0) return workgroups;
-  if (prefix_cost == 0) return 0;
-  const uint64_t eighths = (workgroups / 8 * prefix_cost + (prefix_cost + own_cost) / 2) / (prefix_cost + own_cost);
-  const uint32_t n = (uint32_t)(eighths < 1 ? 1 : (eighths > workgroups / 8 - 1 ? workgroups / 8 - 1 : eighths));
-  return 8 * n;
-}
-
 // Workspace: parts of the prefixes' axis, parts of the other, rows kept whole of either, and where both begin.
 struct SharedSpace {
   size_t own_parts, prefix_kept, own_kept, prefix_begins, own_begins, bytes;

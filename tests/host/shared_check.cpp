@@ -14,16 +14,6 @@ using namespace apbv;
   } while (0)
 
 int main() {
-  // both axes get workgroups where both have tiles, in multiples of eight, and all workgroups are someone's
-  for (uint32_t w : {16u, 256u, 512u})
-    for (uint64_t a : {0ull, 1ull, 5ull, 1000ull, 6442450944ull})
-      for (uint64_t b : {0ull, 1ull, 5ull, 1000ull, 2147418112ull}) {
-        const uint32_t n = shared_split(w, a, b);
-        CHECK(n <= w && n % 8 == 0);
-        if (b == 0) CHECK(n == w);
-        if (a == 0 && b > 0) CHECK(n == 0);
-        if (a > 0 && b > 0) CHECK(n >= 8 && n <= w - 8);
-      }
   // the launches there are: tiles of 16 or 32 rows of the prefix with 16 of the own keys, or of 128 with 16 or 128
   for (int d : {64, 128})
     for (int groups : {1, 2, 7, 64, 4096})
