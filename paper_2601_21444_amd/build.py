@@ -35,6 +35,7 @@ SOURCES = {
     "score_matrix.hip": [],
     "shared_api.hip": [],
     "shared_attention.hip": ["-fno-honor-nans"],
+    "shared_short.hip": ["-fno-honor-nans"],
 }
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -28,8 +28,18 @@ struct SharedPlan {
   CachePlan prefix, own;
   int workgroups;
   int join_waves;            // waves that join the parts of a row: 1 or 4
+  bool whole;                // a workgroup for every (group, KV head, 16 rows), with all their keys: prefix.row_tiles of a group
 };
-inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q) {
+//
+// Where the tables hold but a few tiles, a workgroup takes 16 rows and all the keys that they see, without a second launch: a
+// microsecond for every four tiles, where a cut call has its second launch, and whole row tiles of 128 rows for few keys.  How many tiles
+// are few depends on how many such workgroups there are to even them out (us, cut / whole; tiles of the prefix and of the own keys that
+// a row tile sees: 2 requests, 2 / 1 heads of 64, 13 11.2 / 7.5, 24 11.9 / 9.3, 34 11.5 / 11.0, 48 11.9 / 13.0; 8 of 8 / 8 of 128, 12 12.0 /
+// 9.3, 19 12.4 / 11.7, 24 12.1 / 14.0.  128-row tiles: 32 of 16 / 2 heads of 128, 32 workgroups, 19 17.1 / 10.3, 35 18.1 / 15.1, 56 18.4 /
+// 22.3; 128 of 8 / 8, 64 workgroups, 28 22.8 / 17.1, 33 18.9 / 19.3, 49 20.2 / 25.6; 128 of 16 / 2, 128 workgroups, 28 26.3 / 14.5, 56 31.6 / 23.1, 70
+// 31.8 / 26.7; 128 of 28 / 4, 224 workgroups, 56 29.9 / 30.1, 70 35.7 / 29.3).  max_prefix and max_len: keys that a row of the tables holds.
+inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q, int64_t max_prefix,
+                                     int64_t max_len) {
   SharedPlan p;
   p.workgroups = 512;
   p.prefix = choose_cache_plan(n_groups, hq, hkv, d, n_rows, (n_rows + n_groups - 1) / n_groups, 0);
@@ -44,6 +54,14 @@ inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int h
   // a row has as many parts over its prefix as workgroups share it, if the groups are alike
   const int64_t parts = p.workgroups / ((int64_t)n_groups * hkv * p.prefix.row_tiles) + 1;
   p.join_waves = parts > 8 && n_rows * hq <= 2048 ? 4 : 1;
+  const int group = hq / hkv;
+  const int64_t rows = (n_rows + n_groups - 1) / n_groups * group, row_tiles = (rows + 15) / 16;
+  const int64_t per_tile = (int64_t)n_requests * 16 / (n_rows * group) + 1, of_group = (n_requests + n_groups - 1) / n_groups;      // requests
+  const int64_t tiles = (max_prefix + kCacheKeyTile - 1) / kCacheKeyTile + (per_tile < of_group ? per_tile : of_group) * ((max_len + kCacheKeyTile - 1) / kCacheKeyTile);
+  const int64_t groups16 = n_groups * (int64_t)hkv * row_tiles;
+  const int64_t few = p.prefix.rows != kCacheBlockRows ? 22 : (groups16 < 160 ? 24 + groups16 / 4 : 64);
+  p.whole = tiles <= few && groups16 + 2 * (int64_t)hkv * row_tiles <= (int64_t)1 << 22;
+  if (p.whole) p.prefix.row_tiles = (int)row_tiles;
   return p;
 }
 // Workspace: parts of the prefixes' axis, parts of the other, rows kept whole of either, and where both begin.
@@ -65,7 +83,7 @@ inline size_t shared_attention_workspace_bytes(int n_groups, int n_requests, int
   if (n_groups < 1 || n_groups > n_requests || n_rows * (int64_t)hq > 4 * kMaxGroups ||
       cache_attention_workspace_bytes(n_requests, n_rows, hq, hkv, d, max_q) == 0)
     return 0;
-  return shared_space(choose_shared_plan(n_groups, n_requests, hq, hkv, d, n_rows, max_q), n_groups, n_requests, n_rows, hq, d).bytes;
+  return shared_space(choose_shared_plan(n_groups, n_requests, hq, hkv, d, n_rows > 0 ? n_rows : 1, max_q, 0, 0), n_groups, n_requests, n_rows, hq, d).bytes;
 }
 
 }  // namespace apbv

@@ -24,10 +24,13 @@ int main() {
               if (groups > n) continue;
               const int64_t rows = n * each;
               for (int64_t max_q : {(int64_t)0, each, rows, rows + 5}) {
-                const SharedPlan p = choose_shared_plan(groups, n, hkv * g, hkv, d, rows, max_q);
+                const SharedPlan p = choose_shared_plan(groups, n, hkv * g, hkv, d, rows, max_q, 1 << 20, 1 << 20);
                 CHECK(p.prefix.rows == 16 || p.prefix.rows == 32 || p.prefix.rows == kCacheBlockRows);
                 CHECK(p.own.rows == 16 || (p.own.rows == kCacheBlockRows && p.prefix.rows == kCacheBlockRows));
                 CHECK(p.own.row_tiles >= 0 && p.workgroups % 8 == 0);
+                CHECK(!p.whole);
+                const SharedPlan few = choose_shared_plan(groups, n, hkv * g, hkv, d, rows, max_q, 64, 64);
+                if (few.whole) CHECK(few.prefix.row_tiles >= 1 && (groups + 2) * (int64_t)hkv * few.prefix.row_tiles <= 1 << 22 && few.prefix.row_tiles * (int64_t)16 * groups >= rows * g);
                 const SharedSpace s = shared_space(p, groups, n, rows, hkv * g, d);
                 // regions follow one another, hold what is written into them, and start where float4s may
                 CHECK(s.own_parts >= (size_t)p.workgroups * 2 * p.prefix.rows * (d + 3) * 4);

@@ -28,18 +28,19 @@ class Shared:
         self.starts = self.x.starts[self.g:]
         self.of = [next((g for g in range(self.g) if self.members[g] <= b < self.members[g + 1]), None) for b in range(len(self.requests))]
 
-    def args(self, table=None):
-        table = self.x.table if table is None else table
+    def args(self, wide=False):
+        """wide: the tables have room for longer prefixes and requests, so that the call is cut and parts are joined."""
+        table = np.concatenate((self.x.table, np.full((len(self.x.table), 5000 // self.x.page), -1)), 1) if wide else self.x.table
         return (dev_int(table[:self.g].tolist()), dev_int(self.prefixes), dev_int(table[self.g:].tolist()), dev_int([k for _, k in self.requests]))
 
-    def run(self, causal=True, args=None, **kw):
+    def run(self, causal=True, args=None, wide=False, **kw):
         x = self.x
         out = torch.full((x.rows, x.hq, x.d), 77.0, dtype=torch.bfloat16, device="cuda")
         lse = torch.full((x.hq, x.rows), 77.0, device="cuda")
         kw.setdefault("group_starts", dev_int(self.members))
         kw.setdefault("q_starts", dev_int(self.starts))
         kw.setdefault("max_q", max(n for n, _ in self.requests))
-        pt, pl, t, l = args or self.args()
+        pt, pl, t, l = args or self.args(wide)
         apbv.apbv_cache_shared_attention(x.q, x.cache, pt, pl, t, l, x.scale, causal=causal, out=out, lse_out=lse, **kw)
         torch.cuda.synchronize()
         again = torch.full_like(out, 77.0)                            # without the log-sum-exp: the same outputs
@@ -92,19 +93,20 @@ CASES = [
 ]
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("case", range(len(CASES)))
-def test_matches_the_oracle(case, causal):
+def test_matches_the_oracle(case, causal, wide):
     hq, hkv, d, page, groups, alone = CASES[case]
-    print("shared", CASES[case], causal, flush=True)
+    print("shared", CASES[case], causal, wide, flush=True)
     s = Shared(np.random.default_rng((31, case)), hq, hkv, d, page, groups, alone, lead=case % 3, tail=case % 2 * 3)
-    out, lse = s.run(causal)
+    out, lse = s.run(causal, wide=wide)
     s.check(out, lse, causal, f"case {case} causal={causal}")
-    again, lse_again = s.run(causal)
+    again, lse_again = s.run(causal, wide=wide)
     assert torch.equal(out.view(torch.int16), again.view(torch.int16)) and torch.equal(lse, lse_again)
     # max_q changes how the work is cut, not what is computed
     for max_q in (s.x.rows + 1, 0):
-        more, lse_more = s.run(causal, max_q=max_q)
+        more, lse_more = s.run(causal, wide=wide, max_q=max_q)
         s.check(more, lse_more, causal, f"case {case} causal={causal} max_q={max_q}")
 
 
@@ -112,8 +114,9 @@ def test_matches_the_oracle(case, causal):
 def test_equal_groups_without_starts(groups, each, queries):
     rng = np.random.default_rng((32, groups))
     s = Shared(rng, 8, 2, 128, 32, [(100 + 90 * g, [(queries, queries + 17 * i) for i in range(each)]) for g in range(groups)])
-    out, lse = s.run(group_starts=None, q_starts=None, max_q=None)
-    s.check(out, lse, True, "equal groups")
+    for wide in (False, True):
+        out, lse = s.run(group_starts=None, q_starts=None, max_q=None, wide=wide)
+        s.check(out, lse, True, "equal groups")
 
 
 @pytest.mark.parametrize("n_groups,n", [(1, 100), (3, 200), (80, 90), (70, 300)])
@@ -124,8 +127,19 @@ def test_many_requests_and_groups(n_groups, n):
     groups = [(int(rng.choice([0, 16, 65, int(rng.integers(1, 400))])), [(1, int(rng.choice([0, 1, 64, int(rng.integers(1, 200))]))) for _ in range(m)]) for m in sizes]
     print("many", n_groups, n, flush=True)
     s = Shared(rng, 4, 2, 64, 16, groups, (((1, 10),), ((1, 0),)))
-    out, lse = s.run()
-    s.check(out, lse, True, "many")
+    for wide in (False, True):
+        out, lse = s.run(wide=wide)
+        s.check(out, lse, True, "many")
+
+
+def test_requests_of_one_group_in_many_windows():
+    """Rows of a tile that are of requests far apart, with requests of no rows between them."""
+    rng = np.random.default_rng(45)
+    requests = [(int(rng.random() < 0.1), int(rng.integers(0, 60))) for _ in range(400)]
+    s = Shared(rng, 2, 2, 64, 16, [(100, requests), (30, [(3, 40)])], (((0, 5),) * 70 + ((1, 9),), ((2, 17),)))
+    for wide in (False, True):
+        out, lse = s.run(wide=wide)
+        s.check(out, lse, True, "windows")
 
 
 def test_long_prefixes_are_compared_as_a_whole():
@@ -154,8 +168,9 @@ def test_peaked_logits():
         s = Shared(np.random.default_rng((36, int(factor))), 8, 1, 128, 64, [(1500, [(1, 300)] * 3), (70, [(5, 600)])], k_scale=factor)
         s.x.qv *= 0.25
         s.x.q = (s.x.q.float() * 0.25).bfloat16()
-        out, lse = s.run()
-        s.check(out, lse, True, f"keys of scale {factor}")
+        for wide in (False, True):
+            out, lse = s.run(wide=wide)
+            s.check(out, lse, True, f"keys of scale {factor}")
 
 
 def test_keys_on_bad_pages_are_not_there():
@@ -171,8 +186,9 @@ def test_keys_on_bad_pages_are_not_there():
             if r == row:
                 keep[i * 32:(i + 1) * 32] = False
         return keep
-    out, lse = s.run(causal=False)
-    s.check(out, lse, False, "bad pages", kept=kept)
+    for wide in (False, True):
+        out, lse = s.run(causal=False, wide=wide)
+        s.check(out, lse, False, "bad pages", kept=kept)
     assert (out[s.starts[2]] == 0).all() and torch.isneginf(lse[:, s.starts[2]]).all()      # neither prefix nor own keys
 
 
