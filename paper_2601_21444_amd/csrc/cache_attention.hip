@@ -32,7 +32,7 @@ namespace {
 template <int D, int NQ, bool kOnePage, bool kLse, bool kWhole>
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attention_kernel(const CacheAttnParams p) {
   __shared__ FewRowsLds<D, NQ, kWhole> lds;
-  attend_few_rows<D, NQ, kOnePage, kLse, kWhole ? Form::kWhole : Form::kCut>(p, lds, blockIdx.x, (uint32_t)p.workgroups);
+  attend_few_rows<D, NQ, kOnePage, kLse, kWhole ? Form::kWhole : Form::kCut>(p, lds, blockIdx.x, AxisCut{}, Request{});
 }
 
 // kJoin waves per (row of q, head): joins the parts of rows that several workgroups share, and clears the rows without a key.

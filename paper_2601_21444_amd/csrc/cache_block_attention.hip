@@ -23,7 +23,7 @@ namespace {
 template <int D, bool kLse>                                // kLse: as in cache_attention.hip
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_block_attention_kernel(const CacheAttnParams p) {
   __shared__ BlockRowsLds<D> lds;
-  attend_block_rows<D, kLse>(p, lds, blockIdx.x, (uint32_t)p.workgroups);
+  attend_block_rows<D, kLse>(p, lds, blockIdx.x, AxisCut{}, Request{});
 }
 
 }  // namespace

@@ -23,9 +23,9 @@ struct BlockRowsLds {
   __attribute__((aligned(16))) int gone[4][kCacheWaves];   // 16-key blocks that are not there, of a tile modulo 4
 };
 
-// kLse, kKept, `block` of `workgroups`: as in cache_few_rows.h.
+// kLse, kKept, `block`, `cut`: as in cache_few_rows.h.
 template <int D, bool kLse, bool kKept = false, bool kGroups = false, typename P>
-__device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& shared, uint32_t block, uint32_t workgroups) {
+__device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& shared, uint32_t block, const AxisCut& cut, const Request& of_lane) {
   using T = Tile<D, 1, true>;
   constexpr int W = kCacheWaves, R = kCacheBlockRows;
   static_assert(R == 32 * W, "a wave owns 32 rows");
@@ -40,12 +40,23 @@ __device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& s
   if constexpr (kKept) asm volatile("" : "+v"(lane));       // (what follows from it is not kept in registers across the work of the other axis)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hh = lane >> 5;
-  Axis<R, kGroups> axis(p);
-  const uint32_t share = axis.share(p, workgroups);
-  const int wg = axis.my_share(share, block);
-  if (wg < 0) return;
-  uint32_t pos = wg * share;
-  const uint32_t end = share < axis.total - pos ? pos + share : axis.total;
+  typedef Axis<R, kGroups> A;
+  A axis = kKept && p.n_requests <= 64 ? A(p, of_lane) : A(p);
+  uint32_t pos, end, share = 0;
+  int wg;
+  if constexpr (kKept) {
+    const uint32_t die = block % kCutDies, x = block / kCutDies, past = cut_end(cut, die, x);
+    pos = cut_begin(cut, die, x);
+    end = past < axis.total ? past : axis.total;
+    if (pos >= end) return;
+    wg = (int)(die * cut.used + x);
+  } else {
+    share = axis.share(p);
+    wg = axis.my_share(share, block);
+    if (wg < 0) return;
+    pos = wg * share;
+    end = share < axis.total - pos ? pos + share : axis.total;
+  }
   int b = axis.find(p, pos);
   uint32_t begin = axis.begin_of(b);
 
@@ -85,7 +96,12 @@ __device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& s
     const uint32_t rel = pos - begin, item = rel / (uint32_t)rq.tiles;
     const int head = (int)(item / (uint32_t)row_tiles), rt = (int)(item - (uint32_t)head * row_tiles);
     const int t0 = (int)(rel - item * (uint32_t)rq.tiles);
-    if (rel == 0 && wave == 0) axis.template leave_word<kKept>(p, b, begin, share);
+    if (rel == 0 && wave == 0) {
+      if constexpr (kKept)
+        axis.leave_word(p, b, begin, cut);
+      else
+        axis.leave_word(p, b, begin, share);
+    }
     const int t1 = end - pos < (uint32_t)(rq.tiles - t0) ? t0 + (int)(end - pos) : rq.tiles;
     pos += t1 - t0;
 

@@ -25,10 +25,10 @@ struct FewRowsLds {
 
 // kLse: the log-sum-exp is wanted, and the weights are added up before they are rounded, too: their rounded sum, which the
 // output is divided by, would leave it with errors of 2^-9 over the square root of the number of keys.
-// `block` of `workgroups`: which share.
+// `block`: which share; kKept: of this cut, which has it.
 template <int D, int NQ, bool kOnePage, bool kLse, Form kForm, bool kGroups = false, typename P>
 __device__ __forceinline__ void attend_few_rows(const P& p, FewRowsLds<D, NQ, kForm == Form::kWhole>& shared, uint32_t block,
-                                                uint32_t workgroups) {
+                                                const AxisCut& cut, const Request& of_lane) {
   using T = Tile<D, 1>;
   constexpr int W = kCacheWaves, R = 16 * NQ;
   constexpr bool kWhole = kForm == Form::kWhole, kKept = kForm == Form::kKept;
@@ -413,12 +413,22 @@ __device__ __forceinline__ void attend_few_rows(const P& p, FewRowsLds<D, NQ, kF
       __syncthreads();                                     // LDS is free again
     }
   } else {
-    Axis<R, kGroups> axis(p);
-    const uint32_t share = axis.share(p, workgroups);
-    wg = axis.my_share(share, block);
-    if (wg < 0) return;
-    const uint32_t wg_begin = wg * share;
-    const uint32_t wg_end = share < axis.total - wg_begin ? wg_begin + share : axis.total;
+    typedef Axis<R, kGroups> A;
+    A axis = kKept && p.n_requests <= 64 ? A(p, of_lane) : A(p);
+    uint32_t wg_begin, wg_end, share = 0;
+    if constexpr (kKept) {
+      const uint32_t die = block % kCutDies, x = block / kCutDies, past = cut_end(cut, die, x);
+      wg_begin = cut_begin(cut, die, x);
+      wg_end = past < axis.total ? past : axis.total;
+      if (wg_begin >= wg_end) return;
+      wg = (int)(die * cut.used + x);
+    } else {
+      share = axis.share(p);
+      wg = axis.my_share(share, block);
+      if (wg < 0) return;
+      wg_begin = wg * share;
+      wg_end = share < axis.total - wg_begin ? wg_begin + share : axis.total;
+    }
     // a wave's part of the share
     const uint32_t wave_share = (wg_end - wg_begin + W - 1) / W;
     uint32_t pos = wg_begin + wave * wave_share;
@@ -442,7 +452,12 @@ __device__ __forceinline__ void attend_few_rows(const P& p, FewRowsLds<D, NQ, kF
       const uint32_t rel = pos - begin, item = rel / (uint32_t)rq.tiles;
       const int head = (int)(item / (uint32_t)row_tiles), rt = (int)(item - (uint32_t)head * row_tiles);
       const int t0 = (int)(rel - item * (uint32_t)rq.tiles);
-      if (rel == 0) axis.template leave_word<kKept>(p, b, begin, share);
+      if (rel == 0) {
+        if constexpr (kKept)
+          axis.leave_word(p, b, begin, cut);
+        else
+          axis.leave_word(p, b, begin, share);
+      }
       const int t1 = end - pos < (uint32_t)(rq.tiles - t0) ? t0 + (int)(end - pos) : rq.tiles;
       pos += t1 - t0;
       piece(rq, b, head, rt, t0, t1);

@@ -132,6 +132,23 @@ struct Axis {
     group_past = wave_scan(sum);
     total = top(__builtin_amdgcn_readlane(group_past, 63));
   }
+  // Of up to 64 requests: this lane's, or none (asked for without a branch, so that two axes' loads are under way together), and the
+  // axis of what is already there.
+  template <typename P>
+  __device__ __forceinline__ static Request lane_request(const P& p) {
+    const int b = (int)(threadIdx.x & 63);
+    Request r = load(p, b < p.n_requests ? b : p.n_requests - 1);
+    if (b >= p.n_requests) r = Request{0x7fffffff, 0, 0, 0};
+    return r;
+  }
+  template <typename P>
+  __device__ __forceinline__ Axis(const P& p, const Request& of_lane) {
+    base = 0;
+    base_begin = 0;
+    mine = of_lane;
+    past = wave_scan(tiles(p, mine));
+    total = top(__builtin_amdgcn_readlane(past, 63));
+  }
   // Of the rows alone, for find_row: whoever takes a request's first tile leaves word of where it begins.
   struct RowsOnly {};
   template <typename P>
@@ -147,12 +164,18 @@ struct Axis {
     if (b < p.n_requests) group_first = clip(first_row(p, b), p.n_rows);
     group_past = 0;
   }
-  template <bool kAlways = false, typename P>
+  template <typename P>
   __device__ __forceinline__ void leave_word(const P& p, int b, uint32_t begin, uint32_t share) const {
-    if ((kAlways || p.n_requests > 64) && (threadIdx.x & 63) == 0) {
+    if (p.n_requests > 64 && (threadIdx.x & 63) == 0) {
       p.begins[1 + b] = begin;
       if (begin == 0) p.begins[0] = share;
     }
+  }
+  template <typename P>
+  __device__ __forceinline__ void leave_word(const P& p, int b, uint32_t begin, const AxisCut& cut) const {
+    if ((threadIdx.x & 63) != 0) return;
+    p.begins[kCutWords + b] = begin;
+    if (begin == 0) *reinterpret_cast<CutWord*>(p.begins) = cut_word(cut);
   }
   template <typename P>
   __device__ __forceinline__ void group_window(const P& p, int group) {
@@ -171,13 +194,11 @@ struct Axis {
     r.tiles = __builtin_amdgcn_readlane(mine.tiles, b - base);
     return r;
   }
-  // Length of a workgroup's share, of as many as there are.
+  // Length of a workgroup's share.
   template <typename P>
-  __device__ __forceinline__ uint32_t share(const P& p, uint32_t workgroups) const {
-    return cache_share(total, workgroups, (uint32_t)p.short_tiles, (uint32_t)p.least_tiles, (uint32_t)p.share_step);
+  __device__ __forceinline__ uint32_t share(const P& p) const {
+    return cache_share(total, (uint32_t)p.workgroups, (uint32_t)p.short_tiles, (uint32_t)p.least_tiles, (uint32_t)p.share_step);
   }
-  template <typename P>
-  __device__ __forceinline__ uint32_t share(const P& p) const { return share(p, (uint32_t)p.workgroups); }
   // The share of this workgroup, or -1: consecutive shares on one XCD (row tiles of a head read the same keys), which a launch
   // gives its workgroups in turn.
   __device__ __forceinline__ int my_share(uint32_t share, uint32_t block) const {

@@ -175,6 +175,35 @@ constexpr uint32_t cache_share(uint32_t total, uint32_t workgroups, uint32_t sho
   if (q > 3 * share_step) q = (q + share_step - 1) / share_step * share_step;
   return q;
 }
+// An axis that is cut among workgroups which have other work, too (shared_validation.h).  Every die has an equal stretch of `stretch`
+// tiles, which its workgroups take in shares of `share`, the first `full` of them, and of `rest`, the others; `used` of them are
+// needed.  Shares are numbered die after die.
+struct AxisCut {
+  uint32_t stretch, share, rest, full, used;
+};
+constexpr uint32_t kCutDies = 8;
+constexpr int kCutWords = 12;                 // a CutWord: left in front of where the requests begin
+constexpr uint32_t cut_begin(const AxisCut& c, uint32_t die, uint32_t x) {
+  return die * c.stretch + (x <= c.full ? x * c.share : c.full * c.share + (x - c.full) * c.rest);
+}
+constexpr uint32_t cut_end(const AxisCut& c, uint32_t die, uint32_t x) {
+  const uint32_t e = cut_begin(c, die, x) + (x < c.full ? c.share : c.rest), top = (die + 1) * c.stretch;
+  return e < top ? e : top;
+}
+// The number of the share that holds tile `pos`, by reciprocals: (a + 1/2) / b is no nearer to a whole number than 1 / (2 b), and a double's
+// error is smaller (as query_of has it).
+struct CutWord {
+  AxisCut cut;
+  uint32_t pad;
+  double per_stretch, per_share, per_rest;
+};
+constexpr uint32_t cut_divide(uint32_t a, double per_b) { return (uint32_t)(((double)a + 0.5) * per_b); }
+constexpr CutWord cut_word(const AxisCut& c) { return CutWord{c, 0, 1.0 / c.stretch, 1.0 / c.share, 1.0 / c.rest}; }
+constexpr uint32_t cut_share_of(const CutWord& w, uint32_t pos) {
+  const AxisCut& c = w.cut;
+  const uint32_t die = cut_divide(pos, w.per_stretch), at = pos - die * c.stretch, in_full = c.full * c.share;
+  return die * c.used + (at < in_full ? cut_divide(at, w.per_share) : c.full + cut_divide(at - in_full, w.per_rest));
+}
 inline size_t cache_part_bytes(int rows, int d) { return (size_t)rows * (size_t)(d + 3) * sizeof(float); }
 inline size_t cache_parts_bytes(const CachePlan& p, int d) {
   const size_t heads = p.rows != 32 ? 0 : (size_t)kCacheWaves * p.rows * d * sizeof(float);      // pieces that have no room in LDS

@@ -21,16 +21,30 @@ struct LdsOf<D, kCacheBlockRows> {
 };
 
 template <int D, int R, bool kOnePage, bool kLse, bool kGroups, typename P>
-__device__ __forceinline__ void attend(const P& p, typename LdsOf<D, R>::type& lds, uint32_t block, uint32_t workgroups) {
+__device__ __forceinline__ void attend(const P& p, typename LdsOf<D, R>::type& lds, uint32_t block, const AxisCut& cut,
+                                       const Request& of_lane) {
   if constexpr (R == kCacheBlockRows)
-    attend_block_rows<D, kLse, true, kGroups>(p, lds, block, workgroups);
+    attend_block_rows<D, kLse, true, kGroups>(p, lds, block, cut, of_lane);
   else
-    attend_few_rows<D, R / 16, kOnePage, kLse, Form::kKept, kGroups>(p, lds, block, workgroups);
+    attend_few_rows<D, R / 16, kOnePage, kLse, Form::kKept, kGroups>(p, lds, block, cut, of_lane);
 }
 
-// Every workgroup has a share of either axis, or of one of them where they are short: those of the prefixes are dealt from the first
-// workgroup on, those of the own keys from the last.  Half of the workgroups begin with the one and half with the other, so that beside
-// a workgroup that is bound by matrix instructions one runs that is bound by memory, and all end together.
+__device__ __forceinline__ AxisCut uniform(const AxisCut& c) {       // (whole-number divisions leave the scalar registers)
+  auto u = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane(x); };
+  return AxisCut{u(c.stretch), u(c.share), u(c.rest), u(c.full), u(c.used)};
+}
+
+// What a share of `tiles` tiles of own keys costs, in tiles of a prefix: its start, and 64 keys of 16 rows or of a row tile.
+template <int RP, int RO>
+constexpr uint32_t own_cost(uint32_t tiles) {
+  if (RO == kCacheBlockRows) return 2 + tiles;
+  return RP == kCacheBlockRows ? 2 + tiles / 7 : 4 + tiles;
+}
+
+// Every workgroup has a share of either axis, or of one of them where they are short: those of the prefixes are dealt from each die's first
+// workgroup on, those of the own keys from the last, and a workgroup that has own keys takes as much less of the prefixes as they cost.
+// Half of the workgroups begin with the one and half with the other, so that beside a workgroup that is bound by matrix
+// instructions one runs that is bound by memory.
 template <int D, int RP, int RO, bool kOnePage, bool kLse>
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_attention_kernel(const SharedParams) {
   __shared__ union Lds {
@@ -41,19 +55,48 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_attention_kernel(c
   // (arguments are read from where they lie, when they are needed: there are too many for the scalar registers)
   typedef APBV_CONST(SharedParams) Arguments;
   Arguments args = (Arguments)__builtin_amdgcn_kernarg_segment_ptr();
-  const uint32_t workgroups = (uint32_t)args->own.workgroups;
-  bool on_prefix = blockIdx.x < workgroups / 2;
+  constexpr uint32_t workgroups = kSharedWorkgroups;
+  AxisCut of_own, of_prefix;
+  // (in LDS, where all waves write the same, until it is this axis' turn: registers are what there is least of)
+  __shared__ Request of_lanes[2][64];
+  const int lane = threadIdx.x & 63;
+  {
+    typedef Axis<RO> Own;
+    typedef Axis<RP, true> Prefix;
+    uint32_t own_total, prefix_total;
+    if (args->own.n_requests <= 64) {                      // (there are no more groups than requests)
+      const Request prefix_group = Prefix::lane_request(args->prefix), own_request = Own::lane_request(args->own);
+      of_lanes[0][lane] = own_request;
+      of_lanes[1][lane] = prefix_group;
+      own_total = Own(args->own, own_request).total;
+      prefix_total = Prefix(args->prefix, prefix_group).total;
+    } else {
+      own_total = Own(args->own).total;
+      prefix_total = Prefix(args->prefix).total;
+      if (args->prefix.n_requests <= 64) of_lanes[1][lane] = Prefix::lane_request(args->prefix);
+    }
+    of_own = uniform(shared_cut(own_total, workgroups, (uint32_t)args->own.short_tiles, (uint32_t)args->own.least_tiles, 0, 0));
+    of_prefix = uniform(shared_cut(prefix_total, workgroups, (uint32_t)args->prefix.short_tiles, (uint32_t)args->prefix.least_tiles,
+                           own_total > 0 ? of_own.used : 0, own_cost<RP, RO>(of_own.share)));
+  }
+  const int begins_with = blockIdx.x < workgroups / 2 ? 1 : 0;
 #pragma unroll 1
-  for (int turn = 0; turn < 2; ++turn, on_prefix = !on_prefix) {
-    if (turn > 0) __syncthreads();                         // LDS is free again
-    asm volatile("" : "+s"(args));
+  for (int turn = 0; turn < 2; ++turn) {
+    const bool on_prefix = (turn ^ begins_with) != 0;
     const uint32_t block = on_prefix ? blockIdx.x : workgroups - 1 - blockIdx.x;
-    if constexpr (RP == RO)                                // (one body for both)
-      attend<D, RP, kOnePage, kLse, true>(on_prefix ? args->prefix : args->own, lds.prefix, block, workgroups);
-    else if (on_prefix)
-      attend<D, RP, kOnePage, kLse, true>(args->prefix, lds.prefix, block, workgroups);
-    else
-      attend<D, RO, kOnePage, kLse, false>(args->own, lds.own, block, workgroups);
+    if (turn > 0) __syncthreads();                         // LDS is free again
+    const AxisCut cut = {on_prefix ? of_prefix.stretch : of_own.stretch, on_prefix ? of_prefix.share : of_own.share, on_prefix ? of_prefix.rest : of_own.rest,
+                         on_prefix ? of_prefix.full : of_own.full, on_prefix ? of_prefix.used : of_own.used};
+    if (block / kCutDies < cut.used) {
+      Arguments now = args;
+      asm volatile("" : "+s"(now));
+      if constexpr (RP == RO)                              // (one body for both)
+        attend<D, RP, kOnePage, kLse, true>(on_prefix ? now->prefix : now->own, lds.prefix, block, cut, of_lanes[on_prefix ? 1 : 0][lane]);
+      else if (on_prefix)
+        attend<D, RP, kOnePage, kLse, true>(now->prefix, lds.prefix, block, cut, of_lanes[1][lane]);
+      else
+        attend<D, RO, kOnePage, kLse, false>(now->own, lds.own, block, cut, of_lanes[0][lane]);
+    }
   }
 }
 
@@ -79,24 +122,25 @@ __device__ __forceinline__ Parts parts_of(const CacheAttnParams& p, int row, int
   const int mine = base + lane;
   Request rq = {0x7fffffff, 0, 0, 0};
   uint32_t begin = 0;
-  const uint32_t share = p.begins[0];
+  const auto* left = (APBV_CONST(CutWord))p.begins;        // (through the scalar cache)
+  const CutWord word = {{left->cut.stretch, left->cut.share, left->cut.rest, left->cut.full, left->cut.used}, 0, left->per_stretch, left->per_share, left->per_rest};
   if (mine < p.n_requests) {
-    begin = p.begins[1 + mine];
+    begin = p.begins[kCutWords + mine];
     rq = A::load(p, mine);
   }
   const uint64_t before = __builtin_amdgcn_ballot_w64(rq.first <= row);
   const int at = before ? 63 - __builtin_clzll(before) : 0;
   const int first_row = __builtin_amdgcn_readlane(rq.first, at), rows = __builtin_amdgcn_readlane(rq.rows, at), tiles = __builtin_amdgcn_readlane(rq.tiles, at);
-  const uint32_t its_begin = __builtin_amdgcn_readlane(begin, at), each = __builtin_amdgcn_readfirstlane(share > 0 ? share : 1);
+  const uint32_t its_begin = __builtin_amdgcn_readlane(begin, at);
   const int i = row - first_row;
   Parts x;
   x.of_axis = i >= 0 && i * p.group < rows;
   const int r = i * p.group + h % p.group, rt = r / R, row_tiles = (rows + R - 1) / R;
   const uint32_t from = its_begin + (uint32_t)(h / p.group * row_tiles + rt) * (uint32_t)tiles;
   // (requests that overlap, against the contract, may have left no word: whatever it says, reads stay inside the workspace)
-  const uint32_t top = (uint32_t)p.workgroups - 1, first = from / each, last = (from + (uint32_t)tiles - 1) / each;
+  const uint32_t top = (uint32_t)p.workgroups - 1, first = cut_share_of(word, from), last = cut_share_of(word, from + (uint32_t)tiles - 1);
   x.first = (int)(first < top ? first : top);
-  x.count = x.of_axis && tiles > 0 ? (int)(last < top ? last : top) - x.first + 1 : 0;
+  x.count = x.of_axis && tiles > 0 && last >= first ? (int)(last < top ? last : top) - x.first + 1 : 0;
   x.whole = x.count == 1;
   if (x.whole) {
     const int64_t row_at = (int64_t)row * p.hq + h, n = (int64_t)p.n_rows * p.hq;
@@ -215,7 +259,7 @@ void launch_rows(Launcher& launch, const SharedParams& p, int waves) {
   const bool one_page = (1 << p.own.cache.page_log2) >= kCacheKeyTile, lse = p.own.lse != nullptr;
   auto kernel = one_page ? (lse ? shared_attention_kernel<D, RP, RO, true, true> : shared_attention_kernel<D, RP, RO, true, false>)
                          : (lse ? shared_attention_kernel<D, RP, RO, false, true> : shared_attention_kernel<D, RP, RO, false, false>);
-  launch(kernel, dim3((unsigned)p.own.workgroups), dim3(64 * kCacheWaves), 0, p);
+  launch(kernel, dim3(kSharedWorkgroups), dim3(64 * kCacheWaves), 0, p);
   const int64_t rows = (int64_t)p.own.n_rows * p.own.hq;
   if (waves == 4)
     launch(shared_join_kernel<D, RP, RO, 4>, dim3((unsigned)rows), dim3(256), 0, p);

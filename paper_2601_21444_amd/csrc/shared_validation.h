@@ -24,9 +24,9 @@ inline apbv_status validate_shared_attention(const apbv_cache* cache, int n_grou
 
 // How a call is cut: two axes of tiles as in cache_validation.h, one of the groups over their prefixes and one of the requests over
 // their own keys, of both of which every workgroup takes a share.
+constexpr int kSharedWorkgroups = 512;
 struct SharedPlan {
   CachePlan prefix, own;
-  int workgroups;
   int join_waves;            // waves that join the parts of a row: 1 or 4
   bool whole;                // a workgroup for every (group, KV head, 16 rows), with all their keys: prefix.row_tiles of a group
 };
@@ -41,7 +41,6 @@ struct SharedPlan {
 inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q, int64_t max_prefix,
                                      int64_t max_len) {
   SharedPlan p;
-  p.workgroups = 512;
   p.prefix = choose_cache_plan(n_groups, hq, hkv, d, n_rows, (n_rows + n_groups - 1) / n_groups, 0);
   p.own = choose_cache_plan(n_requests, hq, hkv, d, n_rows, max_q, 0);
   // (row tiles of 32 own rows are taken in two of 16, and no row tile of own rows is higher than those of the prefix)
@@ -50,9 +49,9 @@ inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int h
     p.own.rows = 16;
     p.own.row_tiles = (int)((rows + 15) / 16);
   }
-  p.prefix.workgroups = p.own.workgroups = p.workgroups;
+  p.prefix.workgroups = p.own.workgroups = kSharedWorkgroups;
   // a row has as many parts over its prefix as workgroups share it, if the groups are alike
-  const int64_t parts = p.workgroups / ((int64_t)n_groups * hkv * p.prefix.row_tiles) + 1;
+  const int64_t parts = kSharedWorkgroups / ((int64_t)n_groups * hkv * p.prefix.row_tiles) + 1;
   p.join_waves = parts > 8 && n_rows * hq <= 2048 ? 4 : 1;
   const int group = hq / hkv;
   const int64_t rows = (n_rows + n_groups - 1) / n_groups * group, row_tiles = (rows + 15) / 16;
@@ -64,6 +63,36 @@ inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int h
   if (p.whole) p.prefix.row_tiles = (int)row_tiles;
   return p;
 }
+// The cut of an axis of `total` tiles.  `busy` workgroups of each die, the last ones, have work of the other axis that costs as much as
+// `cost` tiles of this one, and take so many fewer.  Where shares would be shorter than short_tiles, half of the workgroups take part.
+constexpr AxisCut shared_cut(uint32_t total, uint32_t workgroups, uint32_t short_tiles, uint32_t least_tiles, uint32_t busy, uint32_t cost) {
+  const uint32_t w = workgroups / kCutDies;
+  AxisCut c = {0, 0, 0, 0, 0};
+  c.stretch = (total + kCutDies - 1) / kCutDies;
+  c.stretch = c.stretch > least_tiles ? c.stretch : least_tiles;
+  busy = busy < w ? busy : w;
+  const uint32_t even = (c.stretch + w - 1) / w;
+  if (even < short_tiles || busy == 0 || busy == w || cost == 0) {      // (all alike)
+    const uint32_t of = even < short_tiles ? w / 2 : w;
+    c.share = (c.stretch + of - 1) / of;
+    c.share = c.share > least_tiles ? c.share : least_tiles;
+    c.rest = c.share;
+    c.full = w;
+  } else {
+    c.full = w - busy;
+    c.share = (uint32_t)((c.stretch + (uint64_t)busy * cost + w - 1) / w);
+    if (c.share < cost + least_tiles) {                    // nothing is left for those
+      c.share = (c.stretch + c.full - 1) / c.full;
+      c.rest = c.share;
+    } else {
+      c.rest = c.share - cost;
+    }
+  }
+  const uint32_t in_full = c.full * c.share;
+  c.used = c.stretch <= in_full ? (c.stretch + c.share - 1) / c.share : c.full + (c.stretch - in_full + c.rest - 1) / c.rest;
+  return c;
+}
+
 // Workspace: parts of the prefixes' axis, parts of the other, rows kept whole of either, and where both begin.
 struct SharedSpace {
   size_t own_parts, prefix_kept, own_kept, prefix_begins, own_begins, bytes;
@@ -75,8 +104,8 @@ inline SharedSpace shared_space(const SharedPlan& p, int n_groups, int n_request
   s.prefix_kept = s.own_parts + cache_parts_bytes(p.own, d);
   s.own_kept = s.prefix_kept + kept;
   s.prefix_begins = s.own_kept + kept;
-  s.own_begins = s.prefix_begins + align256(((size_t)n_groups + 1) * sizeof(uint32_t));
-  s.bytes = s.own_begins + align256(((size_t)n_requests + 1) * sizeof(uint32_t));
+  s.own_begins = s.prefix_begins + align256(((size_t)n_groups + kCutWords) * sizeof(uint32_t));
+  s.bytes = s.own_begins + align256(((size_t)n_requests + kCutWords) * sizeof(uint32_t));
   return s;
 }
 inline size_t shared_attention_workspace_bytes(int n_groups, int n_requests, int64_t n_rows, int hq, int hkv, int d, int64_t max_q) {
