@@ -229,37 +229,29 @@ __global__ __launch_bounds__(256) void rotate_kernel(const TurnParams p) {
 
 // ---- keys and values for the cache: eight elements a lane, as cache_store_kernel
 
-// float64 elements of a block (its other lanes hold the rest) -> eight codes, and the block's scale byte.
+// float64 elements of a block (its other lanes hold the rest) -> eight codes, and the block's scale byte.  The upper word of an element, with
+// its last bit set where anything lies behind it, is on the same side of every border (all have zeros there) as the element.
 __device__ __forceinline__ uint32_t encode64(const double (&x)[8], uint32_t& scale) {
-  constexpr uint64_t kAbs = ~(1ull << 63), kInf = 0x7ff0000000000000ull, kLargest = 0x47efe00000000000ull;      // the largest finite bf16
-  uint64_t u[8], m = 0;
+  constexpr uint32_t kSign = 0x80000000u, kInf = 0x7ff00000u, kLargest = 0x47efe000u;      // the largest finite bf16
+  uint32_t u[8], m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    u[i] = __builtin_bit_cast(uint64_t, x[i]);
-    const uint64_t a = u[i] & kAbs;
-    u[i] = a > kInf ? 0ull : (a > kLargest ? (u[i] & ~kAbs) | kLargest : u[i]);
-    const uint64_t b = u[i] & kAbs;
-    m = m > b ? m : b;
+    const uint64_t bits = __builtin_bit_cast(uint64_t, x[i]);
+    const uint32_t hi = (uint32_t)(bits >> 32) | ((uint32_t)bits != 0u ? 1u : 0u);
+    uint32_t a = hi & ~kSign;
+    a = a > kInf ? 0u : a;                                 // (not a number: zero)
+    a = a < kLargest ? a : kLargest;
+    m = m > a ? m : a;
+    u[i] = (hi & kSign) | a;
   }
-  auto over_quad = [&](auto ctrl) {
-    constexpr int kCtrl = decltype(ctrl)::value;
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)m, kCtrl, 0xf, 0xf, false);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(m >> 32), kCtrl, 0xf, 0xf, false);
-    const uint64_t y = (uint64_t)hi << 32 | lo;
-    m = m > y ? m : y;
-  };
-  over_quad(std::integral_constant<int, 0xB1>{});
-  over_quad(std::integral_constant<int, 0x4E>{});
-  int e = (int)(m >> 52) - 1023 + 127 - 2 + ((m & 0xfffffffffffffull) > 0xc000000000000ull ? 1 : 0);      // one more from 1.75 * 2^n on
+  m = quad_max(m);
+  int e = (int)(m >> 20) - 1023 + 127 - 2 + ((m & 0xfffffu) > 0xc0000u ? 1 : 0);      // one more from 1.75 * 2^n on
   e = e < 2 ? 2 : (e > 252 ? 252 : e);
   scale = (uint32_t)e;
   const float s = __uint_as_float((uint32_t)e << 23);
   float f[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t hi = (uint32_t)(u[i] >> 32) | ((uint32_t)u[i] != 0u ? 1u : 0u);
-    f[i] = (float)__builtin_bit_cast(double, (uint64_t)hi << 32);
-  }
+  for (int i = 0; i < 8; ++i) f[i] = (float)__builtin_bit_cast(double, (uint64_t)u[i] << 32);
   uint32_t c = 0;
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[0], f[1], s, 0);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f[2], f[3], s, 1);
