@@ -2,8 +2,17 @@
 //
 // The rows of a group are one problem over its prefix, as many rows as its requests have together: the prefix is read and converted once
 // for up to 128 of them, and what it costs is matrix instructions, not bytes.  The rows of a request over its own keys are the problem of
-// cache_attention.hip.  Both lie on axes of tiles of their own, cut into equal shares, in one launch.  A row's parts, of either
+// cache_attention.hip.  Both lie on axes of tiles of their own, cut into shares, in one launch.  A row's parts, of either
 // axis, are left in float32 and joined by a second launch.
+//
+// Bound, behind long prefixes, by what a SIMD issues (cache_block_attention.hip): 64 questions of 16 / 2 heads of 128 behind 133120 keys
+// take 91 us, of which the first launch is 82 (70 GFLOP, 850 TFLOP/s: matrix instructions under way in 44 % of the cycles, vector
+// instructions in 39 % more, hardly any of the one beside the other) and the second, which reads 34 MB of parts, 9; the same 64 rows as one
+// request of apbv_cache_attention, without own keys, take 90.  256 requests of 28 / 4 heads behind 32768 keys, 65 to 2048 of their own
+// 161 (122 GFLOP and 75 MB of own keys), as one request without them 136.  Tried and not kept (us, so / then): waves of 64 rows, one a SIMD
+// with 512 registers, which read half of the LDS bytes, 90 / 99 and 136 / 144 (a lone wave's matrix and vector instructions do not
+// overlap either, and 90 moves between the register files come with every 32 keys); workgroups for the one axis or the other by
+// what they cost 205 / 238 (300 requests behind 40000 keys, up to 300 of their own).
 #include "cache_block_rows.h"
 #include "cache_few_rows.h"
 #include "shared.h"
@@ -42,9 +51,9 @@ constexpr uint32_t own_cost(uint32_t tiles) {
 }
 
 // Every workgroup has a share of either axis, or of one of them where they are short: those of the prefixes are dealt from each die's first
-// workgroup on, those of the own keys from the last, and a workgroup that has own keys takes as much less of the prefixes as they cost.
-// Half of the workgroups begin with the one and half with the other, so that beside a workgroup that is bound by matrix
-// instructions one runs that is bound by memory.
+// workgroup on, those of the own keys from the last, and a workgroup that has own keys takes as much less of the prefixes as they cost
+// (5 requests of 28 / 4 heads behind 10185 keys 21.4 -> 19.0 us, 64 of 16 / 2 behind 133120 92.8 -> 91.5).  Half of the workgroups begin
+// with the one and half with the other (all with the own keys, 1.00 of the time over 19 calls; all with the prefixes, 1.00).
 template <int D, int RP, int RO, bool kOnePage, bool kLse>
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_attention_kernel(const SharedParams) {
   __shared__ union Lds {
