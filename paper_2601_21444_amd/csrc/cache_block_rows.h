@@ -41,7 +41,7 @@ __device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& s
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hh = lane >> 5;
   typedef Axis<R, kGroups> A;
-  A axis = kKept && p.n_requests <= 64 ? A(p, of_lane) : A(p);
+  A axis = kKept ? A(p, of_lane) : A(p);
   uint32_t pos, end, share = 0;
   int wg;
   if constexpr (kKept) {

@@ -414,7 +414,7 @@ __device__ __forceinline__ void attend_few_rows(const P& p, FewRowsLds<D, NQ, kF
     }
   } else {
     typedef Axis<R, kGroups> A;
-    A axis = kKept && p.n_requests <= 64 ? A(p, of_lane) : A(p);
+    A axis = kKept ? A(p, of_lane) : A(p);
     uint32_t wg_begin, wg_end, share = 0;
     if constexpr (kKept) {
       const uint32_t die = block % kCutDies, x = block / kCutDies, past = cut_end(cut, die, x);

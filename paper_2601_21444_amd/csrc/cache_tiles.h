@@ -132,8 +132,7 @@ struct Axis {
     group_past = wave_scan(sum);
     total = top(__builtin_amdgcn_readlane(group_past, 63));
   }
-  // Of up to 64 requests: this lane's, or none (asked for without a branch, so that two axes' loads are under way together), and the
-  // axis of what is already there.
+  // Of up to 64 requests: this lane's, or none (asked for without a branch, so that two axes' loads are under way together).
   template <typename P>
   __device__ __forceinline__ static Request lane_request(const P& p) {
     const int b = (int)(threadIdx.x & 63);
@@ -141,13 +140,24 @@ struct Axis {
     if (b >= p.n_requests) r = Request{0x7fffffff, 0, 0, 0};
     return r;
   }
+  // What a lane has to keep for the axis to be there again without asking memory, and the axis of that.
   template <typename P>
-  __device__ __forceinline__ Axis(const P& p, const Request& of_lane) {
-    base = 0;
-    base_begin = 0;
-    mine = of_lane;
-    past = wave_scan(tiles(p, mine));
-    total = top(__builtin_amdgcn_readlane(past, 63));
+  __device__ __forceinline__ Request of_lane(const P& p) const {
+    return p.n_requests <= 64 ? mine : Request{(int)group_past, 0, 0, 0};
+  }
+  template <typename P>
+  __device__ __forceinline__ Axis(const P& p, const Request& kept) {
+    if (p.n_requests <= 64) {
+      base = 0;
+      base_begin = 0;
+      mine = kept;
+      past = wave_scan(tiles(p, mine));
+      total = top(__builtin_amdgcn_readlane(past, 63));
+    } else {
+      per = (p.n_requests + 63) / 64;
+      group_past = (uint32_t)kept.first;
+      total = top(__builtin_amdgcn_readlane(group_past, 63));
+    }
   }
   // Of the rows alone, for find_row: whoever takes a request's first tile leaves word of where it begins.
   struct RowsOnly {};

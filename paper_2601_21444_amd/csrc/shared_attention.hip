@@ -80,9 +80,12 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_attention_kernel(c
       own_total = Own(args->own, own_request).total;
       prefix_total = Prefix(args->prefix, prefix_group).total;
     } else {
-      own_total = Own(args->own).total;
-      prefix_total = Prefix(args->prefix).total;
-      if (args->prefix.n_requests <= 64) of_lanes[1][lane] = Prefix::lane_request(args->prefix);
+      const Own own_axis(args->own);
+      const Prefix prefix_axis(args->prefix);
+      of_lanes[0][lane] = own_axis.of_lane(args->own);
+      of_lanes[1][lane] = prefix_axis.of_lane(args->prefix);
+      own_total = own_axis.total;
+      prefix_total = prefix_axis.total;
     }
     of_own = uniform(shared_cut(own_total, workgroups, (uint32_t)args->own.short_tiles, (uint32_t)args->own.least_tiles, 0, 0));
     of_prefix = uniform(shared_cut(prefix_total, workgroups, (uint32_t)args->prefix.short_tiles, (uint32_t)args->prefix.least_tiles,
@@ -117,12 +120,13 @@ struct Parts {
   const float *rows, *stat;        // of workgroup 0 in slot 0, or of the row
   int64_t stat_step;
 };
-template <int D, int R, bool kGroups>
+// kFew: there are 64 at most, and nothing is asked for behind a branch, so that the lookups on two axes are under way together.
+template <int D, int R, bool kGroups, bool kFew>
 __device__ __forceinline__ Parts parts_of(const CacheAttnParams& p, int row, int h) {
   typedef Axis<R, kGroups> A;
   const int lane = threadIdx.x & 63;
   int base = 0;
-  if (p.n_requests > 64) {                                 // the last 64th of them that begins at or before the row
+  if (!kFew && p.n_requests > 64) {                        // the last 64th of them that begins at or before the row
     const int per = (p.n_requests + 63) / 64, b = lane * per;
     const uint64_t before = __builtin_amdgcn_ballot_w64(b < p.n_requests && clip(A::first_row(p, b), p.n_rows) <= row);
     base = before ? (63 - __builtin_clzll(before)) * per : 0;
@@ -133,7 +137,10 @@ __device__ __forceinline__ Parts parts_of(const CacheAttnParams& p, int row, int
   uint32_t begin = 0;
   const auto* left = (APBV_CONST(CutWord))p.begins;        // (through the scalar cache)
   const CutWord word = {{left->cut.stretch, left->cut.share, left->cut.rest, left->cut.full, left->cut.used}, 0, left->per_stretch, left->per_share, left->per_rest};
-  if (mine < p.n_requests) {
+  if constexpr (kFew) {
+    begin = p.begins[kCutWords + (mine < p.n_requests ? mine : p.n_requests - 1)];
+    rq = A::lane_request(p);
+  } else if (mine < p.n_requests) {
     begin = p.begins[kCutWords + mine];
     rq = A::load(p, mine);
   }
@@ -177,7 +184,14 @@ __global__ __launch_bounds__(256) void shared_join_kernel(const SharedParams p) 
   const int64_t job = kJoin == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
   if (job >= (int64_t)p.own.n_rows * p.own.hq) return;
   const int row = (int)(job / p.own.hq), h = (int)(job % p.own.hq);
-  const Parts a = parts_of<D, RP, true>(p.prefix, row, h), b = parts_of<D, RO, false>(p.own, row, h);
+  Parts a, b;
+  if (p.own.n_requests <= 64) {                            // (there are no more groups than requests)
+    a = parts_of<D, RP, true, true>(p.prefix, row, h);
+    b = parts_of<D, RO, false, true>(p.own, row, h);
+  } else {
+    a = parts_of<D, RP, true, false>(p.prefix, row, h);
+    b = parts_of<D, RO, false, false>(p.own, row, h);
+  }
   if (!b.of_axis) return;                                  // a row of no request
   const int sub = lane / kLanes, c = lane % kLanes;
   const bool with_lse = p.own.lse != nullptr;
