@@ -19,7 +19,8 @@ extern "C" {
  *   of the first rot_dim elements pair i < rot_dim / 2, (a, b) = (y[i], y[i + rot_dim / 2]), or (y[2i], y[2i + 1]) if `adjacent`,
  *   becomes (a cos t - b sin t, b cos t + a sin t),  t = positions[axis[i]][token] * inv_freq[i];  the other elements stay.
  * Positions with one axis are those of text; with several, time, height and width of a frame's tokens, each pair going with one.
- * Angles are formed and reduced in float64 (the product exact below 2^29), whatever the position: negated positions turn back.
+ * Angles are formed and reduced in float64 (the product exact below 2^29, angles beyond 2^52 unspecified), whatever the position: negated
+ * positions turn back.
  */
 typedef struct {
   const float* inv_freq;    /* [rot_dim / 2]                                                           */
