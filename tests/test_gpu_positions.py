@@ -170,6 +170,26 @@ def test_axes_that_are_the_same_and_no_tokens():
     assert q.shape == (0, 4, 64) and k.shape == (0, 2, 64)
 
 
+def test_rows_beyond_32_bit_offsets():
+    """As many tokens as a call takes, nearly: 2^24 of three heads, strided; rows here and there, the last ones among them."""
+    tokens, hq, hkv, d = (1 << 24) - 3, 2, 1, 64
+    rng = np.random.default_rng(12)
+    print("tokens", tokens, flush=True)
+    block = bf16(rng.standard_normal((1 << 12, hq + hkv, d)))
+    joint = torch.empty(tokens, hq + hkv, d, dtype=torch.bfloat16, device="cuda")
+    joint[:tokens // 4096 * 4096].view(-1, 4096, hq + hkv, d).copy_(block)
+    joint[tokens // 4096 * 4096:] = block[:tokens % 4096]
+    assert joint.numel() > 2 ** 31
+    at = torch.arange(tokens, dtype=torch.int32, device="cuda").mul_(7)
+    inv_freq, weight = frequencies(d), bf16(1.0 + 0.3 * rng.standard_normal(d))
+    rotation = apbv.ApbvRotation(inv_freq, d, k_weight=weight)
+    q, k = apbv.apbv_rotate(joint[:, :hq], joint[:, hq:], at, rotation)
+    looked_at = torch.from_numpy(np.unique(np.concatenate((rng.integers(0, tokens, 300), [0, 11184810, 11184811, tokens - 2, tokens - 1])))).cuda()
+    for x, got, w in ((joint[:, :hq], q, None), (joint[:, hq:], k, weight)):
+        check_rows(got[looked_at], po.rotate(f64(x[looked_at]), f64(at[looked_at])[None], f64(inv_freq), [0] * (d // 2), False,
+                                             None if w is None else f64(w), np.float64(np.float32(1e-6))))
+
+
 # ---- appending to the cache
 
 def slots_of(rng, tokens, n_pages, page, skip):
@@ -222,6 +242,20 @@ def test_append_without_queries_and_slots_out_of_range():
     slots[3], slots[4] = -(1 << 31), (1 << 31) - 1
     assert apbv.apbv_cache_append(cache, None, c.k, c.v, ints(slots), c.positions, c.rotation) is None
     check_append(c, cache, before, slots, 4, 16)
+
+
+def test_append_to_pages_beyond_32_bit_offsets():
+    """A pool of 5 GB, and slots on both sides of 2^32 bytes, the last one among them."""
+    tokens, hkv, d, page, n_pages = 500, 8, 128, 256, 40000
+    print("5 GB pool", flush=True)
+    cache = apbv.apbv_cache_empty(n_pages, hkv, d, page)
+    assert n_pages * cache.k_codes.stride(0) > 2 ** 32
+    c = Case(tokens, 16, hkv, d, d, axes=2, norm=True, seed=13)
+    slots = np.random.default_rng(14).permutation(n_pages * page)[:tokens]
+    slots[0], slots[tokens - 1] = n_pages * page - 1, 0
+    apbv.apbv_cache_append(cache, c.q, c.k, c.v, ints(slots), c.positions, c.rotation)
+    for got, want in zip(apbv.apbv_cache_load(cache, ints(slots)), (c.want(c.k, c.wk)[0], f64(c.v))):
+        assert np.array_equal(f64(got), co.decode(*co.encode(want)))
 
 
 def test_append_of_extreme_values():

@@ -142,6 +142,56 @@ def test_requests_of_one_group_in_many_windows():
         s.check(out, lse, True, "windows")
 
 
+@pytest.mark.parametrize("n_groups", [1, 130, 4096])
+def test_as_many_requests_as_there_may_be(n_groups):
+    rng = np.random.default_rng((46, n_groups))
+    members = np.diff(np.concatenate(([0], np.sort(rng.integers(0, 4097, n_groups - 1)), [4096])))
+    print("4096 requests", n_groups, flush=True)
+    s = Shared(rng, 2, 1, 64, 16, [(int(rng.integers(0, 100)), [(int(rng.random() < 0.8), int(rng.integers(0, 60))) for _ in range(m)]) for m in members])
+    looked_at = sorted({0, 1, 63, 64, 4094, 4095, *(int(b) for b in rng.integers(0, 4096, 150))})
+    for wide in (False, True):
+        out, lse = s.run(wide=wide)
+        s.check(out, lse, True, "4096", only=looked_at)
+        # every request has been written
+        assert torch.isfinite(out.float()).all() and (out.float().abs() < 20).all()
+
+
+def test_more_rows_allowed_than_there_are():
+    """max_q is a bound: the row tiles are those of 128 rows, the results the same to the rounding of the weights and the output."""
+    s = Shared(np.random.default_rng(47), 8, 2, 128, 64, [(3000, [(1, 300)] * 20 + [(2, 2)]), (65, [(1, 70)])])
+    for wide in (False, True):
+        out, lse = s.run(max_q=1000, wide=wide)
+        s.check(out, lse, True, "max_q")
+
+
+@pytest.mark.parametrize("queries", [1, 40])
+def test_pages_beyond_32_bit_offsets(queries):
+    """A pool of 5 GB: pages of a prefix and of requests whose bytes lie behind 2^32, the last one among them; cut, and in one launch."""
+    hkv, hq, d, page, n_pages = 8, 16, 128, 256, 40000
+    print("5 GB pool", queries, flush=True)
+    c = apbv.apbv_cache_empty(n_pages, hkv, d, page)
+    assert n_pages * c.k_codes.stride(0) > 2 ** 32
+    rng = np.random.default_rng(48)
+    pages = np.array([[n_pages - 1, 33000, 0, -1], [32767, -1, -1, -1], [39000, 32768, -1, -1]])
+    keys = [3 * page - 5, 100, page + 77]
+    rows = lambda *shape: torch.from_numpy(rng.standard_normal(shape)).bfloat16().cuda()
+    held = []
+    for row, n in zip(pages, keys):
+        j = np.arange(n)
+        slots = dev_int((row[j // page] * page + j % page).tolist())
+        apbv.apbv_cache_store(c, rows(n, hkv, d), rows(n, hkv, d), slots)
+        held.append([x.double().cpu().numpy() for x in apbv.apbv_cache_load(c, slots)])
+    q = rows(2 * queries, hq, d)
+    qv = q.double().cpu().numpy()
+    for blocks in (4, 60):                                            # (with room for many keys the call is cut)
+        table = dev_int(np.concatenate((pages, np.full((3, blocks - 4), -1)), 1).tolist())
+        out, lse = apbv.apbv_cache_shared_attention(q, c, table[:1], dev_int(keys[:1]), table[1:], dev_int(keys[1:]), 0.088, return_lse=True)
+        for b in range(2):
+            at = slice(b * queries, (b + 1) * queries)
+            ref, ref_lse, spread = co.attention(qv[at], *(np.concatenate((held[0][i], held[1 + b][i])) for i in range(2)), 0.088, True)
+            check(out[at], lse[:, at], ref, ref_lse, spread, f"5 GB pool {blocks} {b}")
+
+
 def test_long_prefixes_are_compared_as_a_whole():
     """The error of a request's rows stays within a step of bf16 in root mean square, which a few lost keys would exceed."""
     s = Shared(np.random.default_rng(34), 8, 1, 128, 64, [(40000, [(1, 500), (1, 3), (1, 64)] * 6)])
