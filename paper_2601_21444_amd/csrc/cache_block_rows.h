@@ -146,16 +146,22 @@ __device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& s
     Codes<D> kc, vc;
     int k_gone = 0;
     bool v_here = true;
+    uint32_t k_code = Codes<D>::code_at(ck, cq), k_scale = Codes<D>::scale_at(ck, cq);
+    uint32_t v_code = Codes<D>::code_at(vk, vq), v_scale = Codes<D>::scale_at(vk, vq);
+    // (the lanes' offsets stay apart from the bases, which are uniform: added up in front of the loop they take twice the registers)
+    auto here_alone = [](uint32_t& code, uint32_t& scale) { asm volatile("" : "+v"(code), "+v"(scale)); };
     auto load_k = [&](const Place& x) {
-      kc.load(p.cache.k_codes + x.codes, p.cache.k_scales + x.scales, 0, 0, ck, cq);
+      here_alone(k_code, k_scale);
+      kc.load(p.cache.k_codes + x.codes, p.cache.k_scales + x.scales, k_code, k_scale);
       k_gone = x.here ? 0 : 1;
     };
     auto load_v = [&](const Place& x) {
-      vc.load(p.cache.v_codes + x.codes, p.cache.v_scales + x.scales, 0, 0, vk, vq);
+      here_alone(v_code, v_scale);
+      vc.load(p.cache.v_codes + x.codes, p.cache.v_scales + x.scales, v_code, v_scale);
       v_here = x.here && vk < x.key_here;
     };
     // (values of keys that are not there may be anything, and a weight of zero would not make them nothing)
-    auto settle_v = [&]() { vc.scale = v_here ? vc.scale : 0u; };
+    auto settle_v = [&]() { vc.scale = v_here ? vc.scale : (uint8_t)0; };
     auto put_k = [&](int slot, int x) { *reinterpret_cast<u32x4*>(k_lds[slot] + (k_put ^ (x << 4))) = kc.values(x); };
     auto put_v = [&](int slot, int x) { *reinterpret_cast<u32x4*>(v_lds[slot] + (v_put ^ (x << 4))) = vc.values(x); };
     auto note_k = [&](int t) { gone_lds[t & 3][wave] = k_gone; };
@@ -184,10 +190,10 @@ __device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& s
     auto hide = [&](f32x16& s, float& lm, int t, int half, int absent) {
       if ((t + 1) * kCacheKeyTile > all || absent != 0) {
         asm volatile("" ::: "memory");                     // (a branch: as selects in every step these cost a seventh of the time)
-        const int jrel = jlast - t * kCacheKeyTile - 32 * half;
+        const int jrel = jlast - t * kCacheKeyTile - 32 * half - 4 * hh;      // (compared with constants, which take no registers)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (8 * (i / 4) + 4 * hh + i % 4 > jrel || (absent >> (2 * half + i / 8) & 1)) s[i] = -INFINITY;
+          if (8 * (i / 4) + i % 4 > jrel || (absent >> (2 * half + i / 8) & 1)) s[i] = -INFINITY;
         lm = lane_max(s);
       }
     };
@@ -283,6 +289,7 @@ __device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& s
             constexpr int m = m0 + J;
             lm = m == 0 ? __builtin_fmaxf(sn[0], sn[1]) : __builtin_fmaxf(lm, __builtin_fmaxf(sn[2 * m], sn[2 * m + 1]));
           });
+          asm volatile("" : "+v"(lm));                     // (it stays here, and does not follow its use behind the branch)
         }
         __builtin_amdgcn_sched_barrier(0);
       });
@@ -344,41 +351,38 @@ __device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& s
       settle_v();
 #pragma unroll
       for (int x = 0; x < kPieces; ++x) {
-        put_k(t0 & 1, x);
-        put_v(t0 & 1, x);
+        put_k(0, x);
+        put_v(0, x);
       }
       note_k(t0);
       kc = next;
       k_gone = place1.here ? 0 : 1;
 #pragma unroll
-      for (int x = 0; x < kPieces; ++x) put_k((t0 & 1) ^ 1, x);
+      for (int x = 0; x < kPieces; ++x) put_k(1, x);
       note_k(t0 + 1);
       next_v = locate(t0 + 2, page2);
       load_k(next_v);
       load_v(place1);
       lds_barrier();
 #pragma unroll
-      for (int kk = 0; kk < KS; ++kk) read_k(t0 & 1, 0, kk);
+      for (int kk = 0; kk < KS; ++kk) read_k(0, 0, kk);
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) s_a = mfma32(kf[kk], qf[kk], kk == 0 ? zero : s_a);
 #pragma unroll
-      for (int kk = 0; kk < KS; ++kk) read_k(t0 & 1, 1, kk);
+      for (int kk = 0; kk < KS; ++kk) read_k(0, 1, kk);
       absent = absent_of(gone_of(t0));
       float lm = lane_max(s_a);
       hide(s_a, lm, t0, 0, absent);
       advance_reference(lm);
+      // (in pairs, with no way out between them: where the paths of one joined those of the other, the compiler waited for codes
+      // that had just been asked for)
       int t = t0;
-      if (t & 1) {
-        body(t, std::integral_constant<int, 1>{});
-        ++t;
-      }
 #pragma unroll 1
-      while (t < t_end) {
+      for (; t + 1 < t_end; t += 2) {
         body(t, std::integral_constant<int, 0>{});
-        if (++t >= t_end) break;
-        body(t, std::integral_constant<int, 1>{});
-        ++t;
+        body(t + 1, std::integral_constant<int, 1>{});
       }
+      if (t < t_end) body(t, std::integral_constant<int, 0>{});
     }
 
     // ---- the rows are done, or this workgroup's part of them: a part that begins the row tile, or one that goes on with it

@@ -239,24 +239,29 @@ template <int D>
 struct Codes {
   static constexpr int kWords = D / 32;
   uint32_t w[kWords];
-  uint32_t scale;
-  // uniform bases, and how far behind them the block lies; this lane's key li of it, quarter lg
-  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int code_step, int scale_step, int li, int lg) {
+  uint8_t scale;             // (a byte: widened as it is loaded, it would be waited for at the end of the loop's turn)
+  // uniform bases, and how far behind them this lane's words and its scale lie
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, uint32_t code_at, uint32_t scale_at) {
     if constexpr (D == 128) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(codes + (uint32_t)(li * 64 + lg * 16) + code_step);
+      const u32x4 x = *reinterpret_cast<const u32x4*>(codes + code_at);
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = x[i];
-      scale = scales[(uint32_t)(li * 4 + lg) + scale_step];
     } else {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(codes + (uint32_t)(li * 32 + lg * 8) + code_step);
+      const u32x2 x = *reinterpret_cast<const u32x2*>(codes + code_at);
       w[0] = x[0];
       w[1] = x[1];
-      scale = scales[(uint32_t)(li * 2 + (lg >> 1)) + scale_step];
     }
+    scale = scales[scale_at];
+  }
+  // ... of key li, quarter lg
+  static __device__ __forceinline__ uint32_t code_at(int li, int lg) { return (uint32_t)(li * (D / 2) + lg * (D / 8)); }
+  static __device__ __forceinline__ uint32_t scale_at(int li, int lg) { return (uint32_t)(D == 128 ? li * 4 + lg : li * 2 + (lg >> 1)); }
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, int code_step, int scale_step, int li, int lg) {
+    load(codes, scales, code_at(li, lg) + code_step, scale_at(li, lg) + scale_step);
   }
   // eight elements as bf16
   __device__ __forceinline__ u32x4 values(int i) const {
-    const float s = __uint_as_float(scale << 23);
+    const float s = __uint_as_float((uint32_t)scale << 23);
     u32x4 x;
     x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 0));
     x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 1));
