@@ -21,7 +21,8 @@ apbv_status apbv_cache_shared_attention(const apbv_cache* cache, int n_groups, i
                                                    table_stride, max_blocks, lengths, q_starts, max_q, softmax_scale, out, lse_out);
   if (st != APBV_OK || q.tokens == 0) return st;
   const SharedPlan plan = choose_shared_plan(n_groups, n_requests, n_q_heads, n_kv_heads, head_dim, q.tokens, max_q,
-                                             max_prefix_blocks * cache->page_size, max_blocks * cache->page_size);
+                                             max_prefix_blocks * cache->page_size, max_blocks * cache->page_size,
+                                             group_starts == nullptr || n_groups == 1);
   const SharedSpace space = shared_space(plan, n_groups, n_requests, q.tokens, n_q_heads, head_dim);
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < space.bytes) return APBV_ERR_WORKSPACE;
   char* const ws = static_cast<char*>(workspace);

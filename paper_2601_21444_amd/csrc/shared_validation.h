@@ -27,39 +27,68 @@ inline apbv_status validate_shared_attention(const apbv_cache* cache, int n_grou
 constexpr int kSharedWorkgroups = 512;
 struct SharedPlan {
   CachePlan prefix, own;
+  size_t prefix_parts, own_parts;      // bytes of the workspace, whatever the tables hold
   int join_waves;            // waves that join the parts of a row: 1 or 4
   bool whole;                // a workgroup for every (group, KV head, 16 rows), with all their keys: prefix.row_tiles of a group
 };
+
+// Row tiles of 16 rows over the prefixes, though the rows would fill some of 32 or 128: a wave works on one by itself, from its start to
+// its part in 2 us and a little more for every tile; a row tile of 128 takes a workgroup 5 us longer to start and to end, but a fourth
+// of the time per row where it is full.  tiles_16, tiles: key tiles of the prefixes that the tables have room for, times row tiles.
 //
-// Where the tables hold but a few tiles, a workgroup takes 16 rows and all the keys that they see, without a second launch: a
-// microsecond for every four tiles, where a cut call has its second launch, and whole row tiles of 128 rows for few keys.  How many tiles
-// are few depends on how many such workgroups there are to even them out (us, cut / whole; tiles of the prefix and of the own keys that
-// a row tile sees: 2 requests, 2 / 1 heads of 64, 13 11.2 / 7.5, 24 11.9 / 9.3, 34 11.5 / 11.0, 48 11.9 / 13.0; 8 of 8 / 8 of 128, 12 12.0 /
-// 9.3, 19 12.4 / 11.7, 24 12.1 / 14.0.  128-row tiles: 32 of 16 / 2 heads of 128, 32 workgroups, 19 17.1 / 10.3, 35 18.1 / 15.1, 56 18.4 /
-// 22.3; 128 of 8 / 8, 64 workgroups, 28 22.8 / 17.1, 33 18.9 / 19.3, 49 20.2 / 25.6; 128 of 16 / 2, 128 workgroups, 28 26.3 / 14.5, 56 31.6 / 23.1, 70
-// 31.8 / 26.7; 128 of 28 / 4, 224 workgroups, 56 29.9 / 30.1, 70 35.7 / 29.3).  max_prefix and max_len: keys that a row of the tables holds.
+// us, row tiles of 128 / of 16 (tiles_16, tiles): 21 requests of 16 / 2 heads of 128 behind 2440 keys 20.6 / 15.4 (858, 156), 8 behind
+// 14128 22.3 / 16.8 (1768, 442), 80 behind 4 prefixes of 2743 29.3 / 21.1 (3440, 688), 37 behind 5 of 14265 39.7 / 32.5 (8920, 2230), 16
+// behind 34286 28.7 / 30.3 (8576, 1072), 11 behind 67889 28.6 / 31.6 (12732, 2122), 27 behind 92268 46.6 / 55.9 (40376, 5768); 43 of 28 /
+// 4 heads behind 8 of 21535, 37 rows, 56.8 / 44.4 (32352, 10784), 213 behind 18062 112 / 145 (106408, 13584).  Heads of 64: 91 of 2 / 1
+// behind 3 of 5753 16.1 / 14.0 (1080, 270), 3 x 49 questions behind 16512 16.0 / 14.2 (2580, 516); 3 x 41 of 8 / 2 behind 10556 18.4 / 20.2
+// (5280, 660), 215 behind 68601 65.7 / 86.6 (115776, 15008).
+// Of 32 / of 16: 17 requests of 8 / 8 heads of 128 behind 3598 18.2 / 14.1 (tiles_16 912), 88 behind 4 of 4933 25.8 / 20.3 (4992), 74
+// behind 3 of 20066 43.7 / 40.3 (15072), 4 of 28 / 4 behind 160000 39.0 / 41.5 (20000); 64: 6 of 8 / 2 behind 2293 12.8 / 11.9 (144), 96 of 2 / 1
+// behind 8 of 19798 19.3 / 18.2 (4960), 48 of 8 / 2 behind 7 of 1500 to 16384 18.0 / 19.3 (7196).
+inline bool low_row_tiles(int d, bool high, int64_t tiles_16, int64_t tiles) {
+  if (!high) return tiles_16 <= (d == 128 ? 16000 : 5000);
+  return tiles_16 <= (d == 128 ? 6000 + tiles * 7 / 2 : 1500 + tiles * 3);
+}
+
+// Where the tables hold but a few tiles, a workgroup takes 16 rows and all the keys that they see, without a second launch: 4 us and
+// 0.37 for every tile, where a cut call takes 12 and more.  How many tiles are few depends on how many such workgroups there are to even them
+// out (us, cut / whole; number of row tiles of 16, tiles of the prefix and of the own keys that one sees): 4 requests of 8 / 2 heads of 64,
+// 2, 14 12.0 / 9.9; 45 of 2 / 1, 6, 25 12.0 / 12.0; 7 of 16 / 2 of 128, 8, 29 13.1 / 15.7; 11, 12, 27 13.4 / 12.8; 36, 36, 46 18.0 / 20.4; 4 x
+// 63 questions of 8 / 2 heads of 64, 64, 27 16.0 / 12.0; 3 x 49 of 16 / 2 of 128, 76, 34 18.0 / 17.0, 4 x 47, 96, 44 23.6 / 19.8; 8 x 51 of
+// 8 / 8, 104, 43 18.8 / 24.9; 87 requests of 28 / 4, 156, 68 33.2 / 29.2, 121, 212, 79 41.0 / 31.6; 80 behind 3 prefixes, 144, 82 31.3 / 111.
+// Groups whose sizes only the device knows have no such workgroups of their own, and the largest keeps its few for long: 37 requests of 2 / 1
+// heads behind 7 prefixes, 17 tiles on average, 12.3 / 17.9, 93 of 8 / 2 behind 4, 12 14.7 / 20.3, 66 of 28 / 4 behind 6, 42 23.4 / 59.5; 31 of
+// 28 / 4 behind 8, 8 15.5 / 12.9.  max_prefix and max_len: keys that a row of the tables holds; even: groups are of equally many requests.
 inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q, int64_t max_prefix,
-                                     int64_t max_len) {
+                                     int64_t max_len, bool even) {
   SharedPlan p;
   p.prefix = choose_cache_plan(n_groups, hq, hkv, d, n_rows, (n_rows + n_groups - 1) / n_groups, 0);
   p.own = choose_cache_plan(n_requests, hq, hkv, d, n_rows, max_q, 0);
+  const int group = hq / hkv;
+  const int64_t rows = (n_rows + n_groups - 1) / n_groups * group, row_tiles = (rows + 15) / 16;
+  const bool high = p.prefix.rows == kCacheBlockRows;
   // (row tiles of 32 own rows are taken in two of 16, and no row tile of own rows is higher than those of the prefix)
-  if (p.own.rows == 32 || p.prefix.rows != kCacheBlockRows) {
-    const int64_t rows = (max_q < n_rows ? max_q : n_rows) * (hq / hkv);
+  auto own_of_16 = [&]() {
     p.own.rows = 16;
-    p.own.row_tiles = (int)((rows + 15) / 16);
+    p.own.row_tiles = (int)(((max_q < n_rows ? max_q : n_rows) * group + 15) / 16);
+  };
+  if (p.own.rows == 32 || !high) own_of_16();
+  p.prefix_parts = cache_parts_bytes(p.prefix, d);
+  p.own_parts = cache_parts_bytes(p.own, d);
+  const int64_t row_tiles_16 = n_groups * (int64_t)hkv * row_tiles, prefix_tiles = (max_prefix + kCacheKeyTile - 1) / kCacheKeyTile;
+  if (p.prefix.rows > 16 && low_row_tiles(d, high, row_tiles_16 * prefix_tiles, n_groups * (int64_t)hkv * p.prefix.row_tiles * prefix_tiles)) {
+    p.prefix.rows = 16;
+    p.prefix.row_tiles = (int)row_tiles;
+    own_of_16();
   }
   p.prefix.workgroups = p.own.workgroups = kSharedWorkgroups;
   // a row has as many parts over its prefix as workgroups share it, if the groups are alike
   const int64_t parts = kSharedWorkgroups / ((int64_t)n_groups * hkv * p.prefix.row_tiles) + 1;
   p.join_waves = parts > 8 && n_rows * hq <= 2048 ? 4 : 1;
-  const int group = hq / hkv;
-  const int64_t rows = (n_rows + n_groups - 1) / n_groups * group, row_tiles = (rows + 15) / 16;
   const int64_t per_tile = (int64_t)n_requests * 16 / (n_rows * group) + 1, of_group = (n_requests + n_groups - 1) / n_groups;      // requests
-  const int64_t tiles = (max_prefix + kCacheKeyTile - 1) / kCacheKeyTile + (per_tile < of_group ? per_tile : of_group) * ((max_len + kCacheKeyTile - 1) / kCacheKeyTile);
-  const int64_t groups16 = n_groups * (int64_t)hkv * row_tiles;
-  const int64_t few = p.prefix.rows != kCacheBlockRows ? 22 : (groups16 < 160 ? 24 + groups16 / 4 : 64);
-  p.whole = tiles <= few && groups16 + 2 * (int64_t)hkv * row_tiles <= (int64_t)1 << 22;
+  const int64_t tiles = prefix_tiles + (per_tile < of_group ? per_tile : of_group) * ((max_len + kCacheKeyTile - 1) / kCacheKeyTile);
+  const int64_t few = !even ? 8 : row_tiles_16 <= 32 ? 24 : row_tiles_16 < 160 ? 16 + row_tiles_16 / 4 : 64;
+  p.whole = tiles <= few && row_tiles_16 + 2 * (int64_t)hkv * row_tiles <= (int64_t)1 << 22;
   if (p.whole) p.prefix.row_tiles = (int)row_tiles;
   return p;
 }
@@ -100,8 +129,8 @@ struct SharedSpace {
 inline SharedSpace shared_space(const SharedPlan& p, int n_groups, int n_requests, int64_t n_rows, int hq, int d) {
   SharedSpace s;
   const size_t kept = align256((size_t)n_rows * (size_t)hq * (size_t)(d + 3) * sizeof(float));
-  s.own_parts = cache_parts_bytes(p.prefix, d);
-  s.prefix_kept = s.own_parts + cache_parts_bytes(p.own, d);
+  s.own_parts = p.prefix_parts;
+  s.prefix_kept = s.own_parts + p.own_parts;
   s.own_kept = s.prefix_kept + kept;
   s.prefix_begins = s.own_kept + kept;
   s.own_begins = s.prefix_begins + align256(((size_t)n_groups + kCutWords) * sizeof(uint32_t));
@@ -112,7 +141,7 @@ inline size_t shared_attention_workspace_bytes(int n_groups, int n_requests, int
   if (n_groups < 1 || n_groups > n_requests || n_rows * (int64_t)hq > 4 * kMaxGroups ||
       cache_attention_workspace_bytes(n_requests, n_rows, hq, hkv, d, max_q) == 0)
     return 0;
-  return shared_space(choose_shared_plan(n_groups, n_requests, hq, hkv, d, n_rows > 0 ? n_rows : 1, max_q, 0, 0), n_groups, n_requests, n_rows, hq, d).bytes;
+  return shared_space(choose_shared_plan(n_groups, n_requests, hq, hkv, d, n_rows > 0 ? n_rows : 1, max_q, 0, 0, true), n_groups, n_requests, n_rows, hq, d).bytes;
 }
 
 }  // namespace apbv

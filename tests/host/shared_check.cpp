@@ -47,13 +47,22 @@ int main() {
               if (groups > n) continue;
               const int64_t rows = n * each;
               for (int64_t max_q : {(int64_t)0, each, rows, rows + 5}) {
-                const SharedPlan p = choose_shared_plan(groups, n, hkv * g, hkv, d, rows, max_q, 1 << 20, 1 << 20);
+                const SharedPlan p = choose_shared_plan(groups, n, hkv * g, hkv, d, rows, max_q, 1 << 30, 1 << 20, true);
                 CHECK(p.prefix.rows == 16 || p.prefix.rows == 32 || p.prefix.rows == kCacheBlockRows);
                 CHECK(p.own.rows == 16 || (p.own.rows == kCacheBlockRows && p.prefix.rows == kCacheBlockRows));
                 CHECK(p.own.row_tiles >= 0 && kSharedWorkgroups % 8 == 0);
                 CHECK(!p.whole);
-                const SharedPlan few = choose_shared_plan(groups, n, hkv * g, hkv, d, rows, max_q, 64, 64);
+                const SharedPlan few = choose_shared_plan(groups, n, hkv * g, hkv, d, rows, max_q, 64, 64, true);
                 if (few.whole) CHECK(few.prefix.row_tiles >= 1 && (groups + 2) * (int64_t)hkv * few.prefix.row_tiles <= 1 << 22 && few.prefix.row_tiles * (int64_t)16 * groups >= rows * g);
+                // whatever the tables hold, the workspace is the same, and tiles of 16 rows fit what it has for higher ones
+                for (int64_t max_prefix : {(int64_t)0, (int64_t)1000, (int64_t)30000, (int64_t)1 << 30})
+                  for (bool even : {false, true}) {
+                    const SharedPlan x = choose_shared_plan(groups, n, hkv * g, hkv, d, rows, max_q, max_prefix, 1 << 20, even);
+                    CHECK(x.prefix.rows <= p.prefix.rows && x.own.rows <= p.own.rows && x.prefix.row_tiles >= 1);
+                    CHECK(x.prefix.rows == p.prefix.rows || (x.prefix.rows == 16 && x.own.rows == 16));
+                    CHECK(shared_space(x, groups, n, rows, hkv * g, d).bytes == shared_space(p, groups, n, rows, hkv * g, d).bytes);
+                    CHECK(x.prefix_parts >= cache_parts_bytes(x.prefix, d) && x.own_parts >= cache_parts_bytes(x.own, d));
+                  }
                 const SharedSpace s = shared_space(p, groups, n, rows, hkv * g, d);
                 // regions follow one another, hold what is written into them, and start where float4s may
                 CHECK(s.own_parts >= (size_t)kSharedWorkgroups * 2 * p.prefix.rows * (d + 3) * 4);

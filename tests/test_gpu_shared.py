@@ -29,8 +29,10 @@ class Shared:
         self.of = [next((g for g in range(self.g) if self.members[g] <= b < self.members[g + 1]), None) for b in range(len(self.requests))]
 
     def args(self, wide=False):
-        """wide: the tables have room for longer prefixes and requests, so that the call is cut and parts are joined."""
-        table = np.concatenate((self.x.table, np.full((len(self.x.table), 5000 // self.x.page), -1)), 1) if wide else self.x.table
+        """wide: the tables have room for longer prefixes and requests, so that the call is cut and parts are joined; so many keys that
+        row tiles are as high as the rows fill."""
+        room = 5000 if wide is True else wide
+        table = np.concatenate((self.x.table, np.full((len(self.x.table), room // self.x.page), -1)), 1) if wide else self.x.table
         return (dev_int(table[:self.g].tolist()), dev_int(self.prefixes), dev_int(table[self.g:].tolist()), dev_int([k for _, k in self.requests]))
 
     def run(self, causal=True, args=None, wide=False, **kw):
@@ -93,7 +95,7 @@ CASES = [
 ]
 
 
-@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("wide", [False, True, 600000])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("case", range(len(CASES)))
 def test_matches_the_oracle(case, causal, wide):
@@ -127,9 +129,22 @@ def test_many_requests_and_groups(n_groups, n):
     groups = [(int(rng.choice([0, 16, 65, int(rng.integers(1, 400))])), [(1, int(rng.choice([0, 1, 64, int(rng.integers(1, 200))]))) for _ in range(m)]) for m in sizes]
     print("many", n_groups, n, flush=True)
     s = Shared(rng, 4, 2, 64, 16, groups, (((1, 10),), ((1, 0),)))
-    for wide in (False, True):
+    for wide in (False, True, 600000):
         out, lse = s.run(wide=wide)
         s.check(out, lse, True, "many")
+
+
+@pytest.mark.parametrize("queries", [1, 9])
+def test_short_groups_of_any_size(queries):
+    """Few enough keys for one launch, groups of none to ten requests, and requests of no group on both sides."""
+    rng = np.random.default_rng((49, queries))
+    sizes = [0, 10, 1, 1, 0, 3, 7, 2, *(int(m) for m in rng.integers(0, 5, 100)), 0, 0, 5]
+    groups = [(int(rng.integers(0, 100)), [(int(rng.integers(0, queries + 1)), int(rng.integers(0, 100))) for _ in range(m)]) for m in sizes]
+    print("short", queries, len(sizes), sum(sizes), flush=True)
+    s = Shared(rng, 4, 2, 64, 16, groups, (((1, 10),) * 3, ((1, 0), (2, 70))), lead=2, tail=3)
+    assert s.args()[0].shape[1] * 16 <= 128                           # two tiles each
+    out, lse = s.run()
+    s.check(out, lse, True, "short")
 
 
 def test_requests_of_one_group_in_many_windows():
@@ -137,7 +152,7 @@ def test_requests_of_one_group_in_many_windows():
     rng = np.random.default_rng(45)
     requests = [(int(rng.random() < 0.1), int(rng.integers(0, 60))) for _ in range(400)]
     s = Shared(rng, 2, 2, 64, 16, [(100, requests), (30, [(3, 40)])], (((0, 5),) * 70 + ((1, 9),), ((2, 17),)))
-    for wide in (False, True):
+    for wide in (False, True, 600000):
         out, lse = s.run(wide=wide)
         s.check(out, lse, True, "windows")
 
@@ -159,7 +174,7 @@ def test_as_many_requests_as_there_may_be(n_groups):
 def test_more_rows_allowed_than_there_are():
     """max_q is a bound: the row tiles are those of 128 rows, the results the same to the rounding of the weights and the output."""
     s = Shared(np.random.default_rng(47), 8, 2, 128, 64, [(3000, [(1, 300)] * 20 + [(2, 2)]), (65, [(1, 70)])])
-    for wide in (False, True):
+    for wide in (False, True, 600000):
         out, lse = s.run(max_q=1000, wide=wide)
         s.check(out, lse, True, "max_q")
 
