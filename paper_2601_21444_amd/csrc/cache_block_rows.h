@@ -143,11 +143,11 @@ __device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& s
       x.scales = (int64_t)((uint64_t)(uint32_t)pg * (uint32_t)p.cache.stride_scales) + at * (uint32_t)(D / 32);
       return x;
     };
-    Codes<D> kc, vc;
+    Codes<D, uint8_t> kc, vc;
     int k_gone = 0;
     bool v_here = true;
-    uint32_t k_code = Codes<D>::code_at(ck, cq), k_scale = Codes<D>::scale_at(ck, cq);
-    uint32_t v_code = Codes<D>::code_at(vk, vq), v_scale = Codes<D>::scale_at(vk, vq);
+    uint32_t k_code = Codes<D, uint8_t>::code_at(ck, cq), k_scale = Codes<D, uint8_t>::scale_at(ck, cq);
+    uint32_t v_code = Codes<D, uint8_t>::code_at(vk, vq), v_scale = Codes<D, uint8_t>::scale_at(vk, vq);
     // (the lanes' offsets stay apart from the bases, which are uniform: added up in front of the loop they take twice the registers)
     auto here_alone = [](uint32_t& code, uint32_t& scale) { asm volatile("" : "+v"(code), "+v"(scale)); };
     auto load_k = [&](const Place& x) {
@@ -341,7 +341,7 @@ __device__ __forceinline__ void attend_block_rows(const P& p, BlockRowsLds<D>& s
       const Place place0 = locate(t0, page0), place1 = locate(t0 + 1, page1);
       load_k(place0);
       load_v(place0);
-      Codes<D> next;
+      Codes<D, uint8_t> next;
       next.load(p.cache.k_codes + place1.codes, p.cache.k_scales + place1.scales, 0, 0, ck, cq);
       {
         const bf16_t* qrow = p.q.ptr + (int64_t)(rq.first + qi) * p.q.st + (int64_t)(head * p.group + row - qi * p.group) * p.q.sh + 8 * hh;

@@ -152,7 +152,7 @@ __device__ __forceinline__ void attend_few_rows(const P& p, FewRowsLds<D, NQ, kF
         for (int kb = 0; kb < 4; ++kb) {
           const int j = t * kCacheKeyTile + 16 * kb;
           const bool gone = now.gone(kb);
-          vc[kb].scale = gone || j + li >= rq.len ? (uint8_t)0 : vc[kb].scale;
+          vc[kb].scale = gone || j + li >= rq.len ? 0u : vc[kb].scale;
 #pragma unroll
           for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll

@@ -235,11 +235,14 @@ struct Axis {
 };
 
 // A 16-key block's codes (16 bytes a lane at head_dim 128, 8 at 64) and scale byte.
-template <int D>
+// S: what the scale is held as.  Where codes are asked for in one turn of a loop and used in the next, behind branches, a byte: widened as it
+// is loaded, it would be waited for at the end of the turn.  Elsewhere, 32 bits (decoding 64 requests of 28 / 4 heads, us: bytes / 32 bits 50.7 /
+// 50.0).
+template <int D, typename S = uint32_t>
 struct Codes {
   static constexpr int kWords = D / 32;
   uint32_t w[kWords];
-  uint8_t scale;             // (a byte: widened as it is loaded, it would be waited for at the end of the loop's turn)
+  S scale;
   // uniform bases, and how far behind them this lane's words and its scale lie
   __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* scales, uint32_t code_at, uint32_t scale_at) {
     if constexpr (D == 128) {

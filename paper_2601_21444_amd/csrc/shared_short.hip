@@ -197,7 +197,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_short_kernel(const
           for (int kb = 0; kb < 4; ++kb) {
             const int j = now_at.tile * kCacheKeyTile + 16 * kb;
             const bool gone = now.gone(kb);
-            vc[kb].scale = gone || j + li >= now_at.len ? (uint8_t)0 : vc[kb].scale;
+            vc[kb].scale = gone || j + li >= now_at.len ? 0u : vc[kb].scale;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (gone || j + 4 * lg + e > jlast) s[kb][e] = -INFINITY;
