@@ -6,13 +6,15 @@
 // axis, are left in float32 and joined by a second launch.
 //
 // Bound, behind long prefixes, by what a SIMD issues (cache_block_attention.hip): 64 questions of 16 / 2 heads of 128 behind 133120 keys
-// take 91 us, of which the first launch is 82 (70 GFLOP, 850 TFLOP/s: matrix instructions under way in 39 % of the cycles, vector
-// instructions in 37 % more, hardly any of the one beside the other) and the second, which reads 34 MB of parts, 9; the same 64 rows as one
-// request of apbv_cache_attention, without own keys, take 90.  256 requests of 28 / 4 heads behind 32768 keys, 65 to 2048 of their own
-// 156 (122 GFLOP and 75 MB of own keys), as one request without them 136.  Tried and not kept (us, so / then): waves of 64 rows, one a SIMD
+// take 89 us, of which the first launch is 80 (70 GFLOP, 880 TFLOP/s: matrix instructions under way in 42 % of the cycles, vector
+// instructions in 37 % more, little of the one beside the other) and the second, which reads 34 MB of parts, 9; the same 64 rows as one
+// request of apbv_cache_attention, without own keys, take 88.  256 requests of 28 / 4 heads behind 32768 keys, 65 to 2048 of their own
+// 153 (122 GFLOP and 75 MB of own keys), as one request without them 132.  Tried and not kept (us, so / then): waves of 64 rows, one a SIMD
 // with 512 registers, which read half of the LDS bytes, 90 / 99 and 136 / 144 (a lone wave's matrix and vector instructions do not
 // overlap either, and 90 moves between the register files come with every 32 keys); workgroups for the one axis or the other by
-// what they cost 205 / 238 (300 requests behind 40000 keys, up to 300 of their own).
+// what they cost 205 / 238 (300 requests behind 40000 keys, up to 300 of their own); parts in the order in which lanes store them, 90.4 / 92.1.
+//
+// Behind shorter prefixes it is bound by its start, the end of the longest share and the join, 12 us with row tiles of 16 rows (shared_validation.h).
 #include "cache_block_rows.h"
 #include "cache_few_rows.h"
 #include "shared.h"
