@@ -3,21 +3,19 @@
 //
 // A workgroup takes 16 rows (query x head of the KV group) of a group and a KV head, and all the keys that they see: the prefix' tiles and
 // behind them those of the own keys of every request that has one of the rows, hidden from the others.  That is one list of tiles,
-// whose quarters the waves take; a wave goes from one segment to the next without a pause, as the next tile is on its way while one is worked on.
-// A tile is worked on as in cache_few_rows.h.  Nothing is cut, so nothing is left to join: bound by the chain of launch, starts, lengths,
-// pages and codes, and a microsecond a tile of a wave: 2 requests of 2 / 1 heads of 64 behind 700 keys, up to 40 of their own, 8.5 us (11 tiles
-// and one a request; cache_attention.hip without a prefix, whose chain is shorter by starts and segments, 6.1).  The rule when it is taken stands
-// in shared_validation.h.
+// of which each wave takes an equal part; a wave goes from one segment to the next without a pause, as the next tile is on its way while one is
+// worked on.  A tile is worked on as in cache_few_rows.h.  Nothing is cut, so nothing is left to join: bound by the chain of launch, starts,
+// lengths, pages and codes, and a microsecond a tile of a wave.  The rule when it is taken, and how many waves there are, stands in shared_validation.h.
 #include "cache_few_rows.h"
 #include "shared.h"
 
 namespace apbv {
 namespace {
 
-template <int D, bool kOnePage, bool kLse>
-__global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_short_kernel(const SharedParams p) {
+template <int D, bool kOnePage, bool kLse, int W>
+__global__ __launch_bounds__(64 * W, 2) void shared_short_kernel(const SharedParams p) {
   using T = Tile<D, 1>;
-  constexpr int W = kCacheWaves, R = 16;
+  constexpr int R = 16;
   constexpr int kWaveLds = T::TILE_BYTES > R * D * 4 ? T::TILE_BYTES : R * D * 4;      // a wave's V tile, later its O
   __shared__ __attribute__((aligned(1024))) unsigned char lds[W][kWaveLds];
   __shared__ float stat[W][3][R];
@@ -263,8 +261,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_short_kernel(const
       }
     }
 
-    // ---- the waves' quarters are put together
-    auto over_quarters = [](float x) {
+    // ---- the waves' parts are put together
+    auto over_lanes = [](float x) {
       {
         auto sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
         x = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
@@ -275,7 +273,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_short_kernel(const
       }
       return x;
     };
-    const float l_tot = over_quarters(l_run), e_tot = kLse ? over_quarters(e_run) : 0.f;
+    const float l_tot = over_lanes(l_run), e_tot = kLse ? over_lanes(e_run) : 0.f;
     f32x4* to_lds = reinterpret_cast<f32x4*>(lds[wave]);
 #pragma unroll
     for (int d = 0; d < T::DBN; ++d) to_lds[li * kChunks + ((4 * d + lg) ^ li)] = o[d];
@@ -318,18 +316,19 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void shared_short_kernel(const
   }
 }
 
-template <int D>
+template <int D, int W>
 auto short_kernel(const SharedParams& p) {
-  if ((1 << p.own.cache.page_log2) >= kCacheKeyTile) return p.own.lse ? shared_short_kernel<D, true, true> : shared_short_kernel<D, true, false>;
-  return p.own.lse ? shared_short_kernel<D, false, true> : shared_short_kernel<D, false, false>;
+  if ((1 << p.own.cache.page_log2) >= kCacheKeyTile) return p.own.lse ? shared_short_kernel<D, true, true, W> : shared_short_kernel<D, true, false, W>;
+  return p.own.lse ? shared_short_kernel<D, false, true, W> : shared_short_kernel<D, false, false, W>;
 }
 
 }  // namespace
 
-apbv_status launch_shared_short(const SharedParams& p, int head_dim, hipStream_t stream) {
+apbv_status launch_shared_short(const SharedParams& p, int head_dim, int waves, hipStream_t stream) {
   Launcher launch(stream);
   const int groups = p.prefix.n_requests + (p.prefix.members ? 2 : 0);
-  launch(head_dim == 128 ? short_kernel<128>(p) : short_kernel<64>(p), dim3((unsigned)(groups * p.own.hkv * p.prefix.row_tiles)), dim3(64 * kCacheWaves), 0, p);
+  auto kernel = waves == 8 ? (head_dim == 128 ? short_kernel<128, 8>(p) : short_kernel<64, 8>(p)) : (head_dim == 128 ? short_kernel<128, 4>(p) : short_kernel<64, 4>(p));
+  launch(kernel, dim3((unsigned)(groups * p.own.hkv * p.prefix.row_tiles)), dim3(64 * waves), 0, p);
   return launch.status();
 }
 

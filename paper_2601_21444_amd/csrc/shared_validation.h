@@ -30,6 +30,7 @@ struct SharedPlan {
   size_t prefix_parts, own_parts;      // bytes of the workspace, whatever the tables hold
   int join_waves;            // waves that join the parts of a row: 1 or 4
   bool whole;                // a workgroup for every (group, KV head, 16 rows), with all their keys: prefix.row_tiles of a group
+  int short_waves;           // waves of such a workgroup
 };
 
 // Row tiles of 16 rows over the prefixes, though the rows would fill some of 32 or 128: a wave works on one by itself, from its start to
@@ -50,15 +51,18 @@ inline bool low_row_tiles(int d, bool high, int64_t tiles_16, int64_t tiles) {
   return tiles_16 <= (d == 128 ? 6000 + tiles * 7 / 2 : 1500 + tiles * 3);
 }
 
-// Where the tables hold but a few tiles, a workgroup takes 16 rows and all the keys that they see, without a second launch: 4 us and
-// 0.37 for every tile, where a cut call takes 12 and more.  How many tiles are few depends on how many such workgroups there are to even them
+// Where the tables hold but a few tiles, a workgroup takes 16 rows and all the keys that they see, without a second launch: 5 us and
+// 0.25 for every tile, where a cut call takes 12 and more.  How many tiles are few depends on how many such workgroups there are to even them
 // out (us, cut / whole; number of row tiles of 16, tiles of the prefix and of the own keys that one sees): 4 requests of 8 / 2 heads of 64,
-// 2, 14 12.0 / 9.9; 45 of 2 / 1, 6, 25 12.0 / 12.0; 7 of 16 / 2 of 128, 8, 29 13.1 / 15.7; 11, 12, 27 13.4 / 12.8; 36, 36, 46 18.0 / 20.4; 4 x
-// 63 questions of 8 / 2 heads of 64, 64, 27 16.0 / 12.0; 3 x 49 of 16 / 2 of 128, 76, 34 18.0 / 17.0, 4 x 47, 96, 44 23.6 / 19.8; 8 x 51 of
-// 8 / 8, 104, 43 18.8 / 24.9; 87 requests of 28 / 4, 156, 68 33.2 / 29.2, 121, 212, 79 41.0 / 31.6; 80 behind 3 prefixes, 144, 82 31.3 / 111.
+// 2, 22 12.4 / 10.5; 8, 4, 48 12.2 / 12.6; 44, 22, 42 13.4 / 10.7; 4 of 8 / 8 of 128, 8, 31 13.5 / 13.3; 7, 8, 33 12.7 / 16.9; 3 x 54 questions,
+// 48, 38 15.7 / 19.8, 10 x 22, 64, 33 17.3 / 17.9; 191 requests, 96, 69 26.9 / 25.2; 65 of 28 / 4, 116, 70 28.3 / 22.2; 10 x 27 questions of 8 /
+// 8, 72, 83 21.8 / 33.5; 154 requests of 16 / 2, 154, 54 30.8 / 21.3; 94 of 28 / 4, 168, 101 33.6 / 35.1, 5 x 46 questions, 208, 34 25.6 / 15.6.
+// Eight waves share the tiles, four where there are more such workgroups than units anyway (us, eight / four waves: 11 requests of 8 / 2 heads
+// of 64, 6, 15 6.8 / 8.0; 154 as above 21.3 / 22.4; 12 x 48 questions, 294, 94 28.8 / 34.5; 196 requests of 28 / 4,
+// 344, 46 36.2 / 33.4, 248, 436, 19 24.8 / 20.2).
 // Groups whose sizes only the device knows have no such workgroups of their own, and the largest keeps its few for long: 37 requests of 2 / 1
-// heads behind 7 prefixes, 17 tiles on average, 12.3 / 17.9, 93 of 8 / 2 behind 4, 12 14.7 / 20.3, 66 of 28 / 4 behind 6, 42 23.4 / 59.5; 31 of
-// 28 / 4 behind 8, 8 15.5 / 12.9.  max_prefix and max_len: keys that a row of the tables holds; even: groups are of equally many requests.
+// heads behind 7 prefixes, 17 tiles on average, 12.3 / 17.9 (four waves), 93 of 8 / 2 behind 4, 12 14.7 / 20.3, 66 of 28 / 4 behind
+// 6, 42 23.4 / 59.5; 31 of 28 / 4 behind 8, 8 15.5 / 12.9.  max_prefix and max_len: keys that a row of the tables holds; even: groups are of equally many requests.
 inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q, int64_t max_prefix,
                                      int64_t max_len, bool even) {
   SharedPlan p;
@@ -87,8 +91,10 @@ inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int h
   p.join_waves = parts > 8 && n_rows * hq <= 2048 ? 4 : 1;
   const int64_t per_tile = (int64_t)n_requests * 16 / (n_rows * group) + 1, of_group = (n_requests + n_groups - 1) / n_groups;      // requests
   const int64_t tiles = prefix_tiles + (per_tile < of_group ? per_tile : of_group) * ((max_len + kCacheKeyTile - 1) / kCacheKeyTile);
-  const int64_t few = !even ? 8 : row_tiles_16 <= 32 ? 24 : row_tiles_16 < 160 ? 16 + row_tiles_16 / 4 : 64;
+  const int64_t more = row_tiles_16 > 48 ? (row_tiles_16 - 48) * 7 / 10 : 0, some = (d == 128 ? 24 : 32) + more;
+  const int64_t few = !even ? 8 : some < 80 ? some : 80;
   p.whole = tiles <= few && row_tiles_16 + 2 * (int64_t)hkv * row_tiles <= (int64_t)1 << 22;
+  p.short_waves = row_tiles_16 <= 320 ? 8 : 4;
   if (p.whole) p.prefix.row_tiles = (int)row_tiles;
   return p;
 }
