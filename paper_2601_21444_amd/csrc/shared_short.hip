@@ -5,7 +5,7 @@
 // behind them those of the own keys of every request that has one of the rows, hidden from the others.  That is one list of tiles,
 // of which each wave takes an equal part; a wave goes from one segment to the next without a pause, as the next tile is on its way while one is
 // worked on.  A tile is worked on as in cache_few_rows.h.  Nothing is cut, so nothing is left to join: bound by the chain of launch, starts,
-// lengths, pages and codes, and a microsecond a tile of a wave.  The rule when it is taken, and how many waves there are, stands in shared_validation.h.
+// lengths, pages and codes, and a microsecond a tile of a wave (2 requests of 2 / 1 heads of 64 behind 700 keys, two tiles a wave, 7.9 us).  The rule when it is taken, and how many waves there are, stands in shared_validation.h.
 #include "cache_few_rows.h"
 #include "shared.h"
 
