@@ -51,6 +51,20 @@ inline bool low_row_tiles(int d, bool high, int64_t tiles_16, int64_t tiles) {
   return tiles_16 <= (d == 128 ? 6000 + tiles * 7 / 2 : 1500 + tiles * 3);
 }
 
+// How many workgroups share a row over one axis, if all of its row tiles have as many key tiles as the tables have room for.  A row is
+// joined by four waves where it has many parts and there are not many rows (us, one wave / four; parts, rows x query heads: 4 requests of 2 / 1
+// heads of 64 behind 89171 keys 22.1 / 14.7 (256, 8), 2 of 28 / 4 of 128 behind 10897 17.5 / 14.1 (88, 56), 14 of 16 / 2 behind 78298 38.7 / 32.3
+// (257, 224), 18 behind 13101 21.3 / 20.7 (16, 288), 75 behind 15930 38.2 / 37.6 (27, 1200); 70 of 8 / 2 of 64 behind 3527 14.5 / 15.4 (9, 560),
+// 51 of 16 / 2 of 128 behind 4 of 1211 16.3 / 17.8 (8, 816), 70 of 28 / 4 behind 7 of 1632 22.9 / 27.4 (5, 1960), 235 of 8 / 2 of 64 behind 6037 26.2 /
+// 30.0 (18, 1880)).
+inline int64_t parts_of_a_row(const CachePlan& p, int64_t units, int64_t tiles) {
+  const int64_t total = units * p.row_tiles * tiles;
+  int64_t share = (total + kSharedWorkgroups - 1) / kSharedWorkgroups;
+  if (share < p.short_tiles) share = (total + kSharedWorkgroups / 2 - 1) / (kSharedWorkgroups / 2);
+  if (share < p.least_tiles) share = p.least_tiles;
+  return tiles / share + 1;
+}
+
 // Where the tables hold but a few tiles, a workgroup takes 16 rows and all the keys that they see, without a second launch: 5 us and
 // 0.25 for every tile, where a cut call takes 12 and more.  How many tiles are few depends on how many such workgroups there are to even them
 // out (us, cut / whole; number of row tiles of 16, tiles of the prefix and of the own keys that one sees): 4 requests of 8 / 2 heads of 64,
@@ -86,11 +100,11 @@ inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int h
     own_of_16();
   }
   p.prefix.workgroups = p.own.workgroups = kSharedWorkgroups;
-  // a row has as many parts over its prefix as workgroups share it, if the groups are alike
-  const int64_t parts = kSharedWorkgroups / ((int64_t)n_groups * hkv * p.prefix.row_tiles) + 1;
-  p.join_waves = parts > 8 && n_rows * hq <= 2048 ? 4 : 1;
+  const int64_t own_tiles = (max_len + kCacheKeyTile - 1) / kCacheKeyTile;
+  const int64_t parts = parts_of_a_row(p.prefix, n_groups * (int64_t)hkv, prefix_tiles) + parts_of_a_row(p.own, n_requests * (int64_t)hkv, own_tiles);
+  p.join_waves = parts > 15 && n_rows * hq <= 1200 ? 4 : 1;
   const int64_t per_tile = (int64_t)n_requests * 16 / (n_rows * group) + 1, of_group = (n_requests + n_groups - 1) / n_groups;      // requests
-  const int64_t tiles = prefix_tiles + (per_tile < of_group ? per_tile : of_group) * ((max_len + kCacheKeyTile - 1) / kCacheKeyTile);
+  const int64_t tiles = prefix_tiles + (per_tile < of_group ? per_tile : of_group) * own_tiles;
   const int64_t more = row_tiles_16 > 48 ? (row_tiles_16 - 48) * 7 / 10 : 0, some = (d == 128 ? 24 : 32) + more;
   const int64_t few = !even ? 8 : some < 80 ? some : 80;
   p.whole = tiles <= few && row_tiles_16 + 2 * (int64_t)hkv * row_tiles <= (int64_t)1 << 22;
