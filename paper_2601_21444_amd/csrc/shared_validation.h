@@ -74,9 +74,10 @@ inline int64_t parts_of_a_row(const CachePlan& p, int64_t units, int64_t tiles) 
 // Eight waves share the tiles, four where there are more such workgroups than units anyway (us, eight / four waves: 11 requests of 8 / 2 heads
 // of 64, 6, 15 6.8 / 8.0; 154 as above 21.3 / 22.4; 12 x 48 questions, 294, 94 28.8 / 34.5; 196 requests of 28 / 4,
 // 344, 46 36.2 / 33.4, 248, 436, 19 24.8 / 20.2).
-// Groups whose sizes only the device knows have no such workgroups of their own, and the largest keeps its few for long: 37 requests of 2 / 1
-// heads behind 7 prefixes, 17 tiles on average, 12.3 / 17.9 (four waves), 93 of 8 / 2 behind 4, 12 14.7 / 20.3, 66 of 28 / 4 behind
-// 6, 42 23.4 / 59.5; 31 of 28 / 4 behind 8, 8 15.5 / 12.9.  max_prefix and max_len: keys that a row of the tables holds; even: groups are of equally many requests.
+// Groups whose sizes only the device knows have no such workgroups of their own, and the largest keeps its few for long: 8 requests of 8 / 8 heads
+// of 128 behind 5 prefixes, 10 tiles on average, 13.3 / 7.3, 87 of 28 / 4 behind 2, 10 17.5 / 13.8, 33 of 16 / 2 behind 2, 11 13.9 / 14.8, 60 of 8 /
+// 8 behind 7, 18 13.5 / 24.2, 92 behind 4, 37 17.7 / 30.0.
+// max_prefix and max_len: keys that a row of the tables holds; even: groups are of equally many requests.
 inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q, int64_t max_prefix,
                                      int64_t max_len, bool even) {
   SharedPlan p;
@@ -106,7 +107,7 @@ inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int h
   const int64_t per_tile = (int64_t)n_requests * 16 / (n_rows * group) + 1, of_group = (n_requests + n_groups - 1) / n_groups;      // requests
   const int64_t tiles = prefix_tiles + (per_tile < of_group ? per_tile : of_group) * own_tiles;
   const int64_t more = row_tiles_16 > 48 ? (row_tiles_16 - 48) * 7 / 10 : 0, some = (d == 128 ? 24 : 32) + more;
-  const int64_t few = !even ? 8 : some < 80 ? some : 80;
+  const int64_t few = !even ? 10 : some < 80 ? some : 80;
   p.whole = tiles <= few && row_tiles_16 + 2 * (int64_t)hkv * row_tiles <= (int64_t)1 << 22;
   p.short_waves = row_tiles_16 <= 320 ? 8 : 4;
   if (p.whole) p.prefix.row_tiles = (int)row_tiles;
