@@ -68,13 +68,14 @@ __device__ __forceinline__ void for_turns(const Rotation& r, int64_t t0, int tok
   const float inv_freq = r.inv_freq[pair];
   for (int t = threadIdx.x / kPairs; t < tokens; t += 256 / kPairs) f(t, pair, turn_of(positions[t], inv_freq));
 }
-// 1 / sqrt(x): the instruction's 24 bits, doubled by a Newton step for each that is asked for.
+// 1 / sqrt(x): the instruction's 24 bits, doubled by a Newton step for each that is asked for; of infinity, which a step would make
+// infinity times zero, zero.
 template <int kSteps>
 __device__ __forceinline__ double inv_sqrt(double x) {
   double y = __builtin_amdgcn_rsq(x);
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) y = __builtin_fma(y * 0.5, __builtin_fma(-x * y, y, 1.0), y);
-  return y;
+  return x == __builtin_inf() ? 0.0 : y;
 }
 
 __device__ __forceinline__ float low(uint32_t x) { return __uint_as_float(x << 16); }
@@ -172,15 +173,29 @@ __device__ __forceinline__ void turn_rows_of(const TurnParams& p, uint32_t group
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = __builtin_fma((double)y[s][i], (double)y[s][i], sum);
       sum = group_sum<L>(sum);
-      const float scale = (float)inv_sqrt<1>(__builtin_fma(sum, 1.0 / D, p.rot.eps));
+      const double inv = inv_sqrt<1>(__builtin_fma(sum, 1.0 / D, p.rot.eps));
+      const float scale = (float)inv;
+      auto weight = [&](int s, int i) { return is_q ? wq[s][i] : wk[s][i]; };
+      if (scale > 0x1p-60f && scale < 0x1p60f) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t w = is_q ? wq[s][i] : wk[s][i];
-          y[s][2 * i] *= scale * low(w);
-          y[s][2 * i + 1] *= scale * high(w);
-        }
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = weight(s, i);
+            y[s][2 * i] *= scale * low(w);
+            y[s][2 * i + 1] *= scale * high(w);
+          }
+      } else {                                             // rows near the ends of bf16's range, in float64: the scale, or
+                                                           // its product with a weight, may be no normal float32
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = weight(s, i);
+            y[s][2 * i] = (float)(y[s][2 * i] * (inv * low(w)));
+            y[s][2 * i + 1] = (float)(y[s][2 * i + 1] * (inv * high(w)));
+          }
+      }
     }
     if (turned) {
       const float* table = lds + (live[u] ? token[u] : 0) * 2 * half;
