@@ -38,7 +38,8 @@ typedef struct {
  *   q [tokens, n_q_heads, head_dim], k [tokens, n_kv_heads, head_dim] bf16, any strides of apbv_tensor (a projection's joint output);
  *              one of them may be left out (0 tokens)
  *   positions  [n_axes, tokens] int32, axes position_stride elements apart (0: all axes the same)
- *   q_out, k_out   bf16, dense; may be q or k itself where that is dense.  Not read where q or k is left out
+ *   q_out, k_out   bf16, dense; q_out may be q itself and k_out k itself where that is dense (else they overlap neither inputs nor each
+ *              other: an output that begins where the other or the other's input does is refused).  Not read where q or k is left out
  * Arithmetic: float32 (the sum of squares and the angles in float64), rounded once, to bf16.  No tokens: nothing is done.
  * Supported: head_dim in {64, 128}; tokens <= 2^24; tokens * (n_q_heads + n_kv_heads) below 2^29.
  */
@@ -49,7 +50,7 @@ apbv_status apbv_rotate(int n_q_heads, int n_kv_heads, int head_dim, const apbv_
  * A step's queries, keys and values [tokens, heads, head_dim]: queries as apbv_rotate leaves them, in q_out; keys, normed and turned,
  * and values into the cache, token t at slots[t].  Slots are as in apbv_cache_store: one outside [0, n_pages * page_size) (-1: padding)
  * is skipped, its query is turned all the same; what a slot named twice holds is unspecified.
- *   q_out   bf16, dense; may be q itself where that is dense
+ *   q_out   bf16, dense; may be q itself where that is dense, not k or v (refused)
  * Keys are formed in float64 and rounded once, to the codes of the cache (a key that apbv_rotate has rounded to bf16 and
  * apbv_cache_store then stores may be held one code away); a NaN is stored as zero, what lies beyond the largest finite bf16 as that.
  * Queries may be left out (0 tokens: keys and values alone).

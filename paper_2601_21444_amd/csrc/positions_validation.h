@@ -75,6 +75,8 @@ inline apbv_status validate_rotate(int hq, int hkv, int d, const apbv_rotation* 
   if ((st = check_turned(k, hkv, d, k_out)) != APBV_OK) return st;
   if (q.tokens != 0 && k.tokens != 0 && q.tokens != k.tokens) return APBV_ERR_SHAPE;
   if (q.tokens == 0 && k.tokens == 0) return APBV_OK;
+  // (each output may be its own input, which a thread reads before it writes; the other's would be written before it is read)
+  if (q.tokens != 0 && k.tokens != 0 && (q_out == k_out || q_out == k.ptr || k_out == q.ptr)) return APBV_ERR_SHAPE;
   if (q.tokens * hq + k.tokens * hkv >= (int64_t)1 << 29) return APBV_ERR_UNSUPPORTED;
   return check_positions(positions, stride);
 }
@@ -88,6 +90,7 @@ inline apbv_status validate_cache_append(const apbv_cache* cache, int hq, int hk
   if ((st = check_turned(q, hq, d, q_out)) != APBV_OK) return st;
   if (q.tokens != 0 && q.tokens != k.tokens) return APBV_ERR_SHAPE;
   if (k.tokens == 0) return APBV_OK;
+  if (q.tokens != 0 && (q_out == k.ptr || q_out == v.ptr)) return APBV_ERR_SHAPE;
   if (q.tokens * hq + k.tokens * hkv >= (int64_t)1 << 29) return APBV_ERR_UNSUPPORTED;
   if (k.tokens * hkv > (int64_t)1 << 26) return APBV_ERR_UNSUPPORTED;      // (below 2^24 workgroups, then: tests/host/positions_check.cpp)
   return check_positions(positions, stride);

@@ -103,7 +103,7 @@ def apbv_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions:
                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Norms and turns the rows of ``q [tokens, Hq, d]`` and ``k [tokens, Hkv, d]`` (either may be None) by ``positions``
     ``[tokens]`` or ``[axes, tokens]`` int32; see apbv_rotate in include/apbv_positions.h.  Returns ``(q_out, k_out)``, dense; an output
-    may be its input, where that is dense."""
+    may be its own input, where that is dense."""
     lib = load_library()
     if stream is None and type(rotation) is ApbvRotation:
         st = binding._native.rotate(q, k, positions, rotation._plan, q_out, k_out)
