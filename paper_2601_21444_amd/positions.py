@@ -35,7 +35,8 @@ class ApbvRotation:
 
     ``inv_freq [rot_dim / 2]`` float32: a frequency per pair.  ``axis``: the axis of the positions that each pair goes with (without it
     there is one).  ``adjacent``: pairs are neighbours, not ``rot_dim / 2`` elements apart.  ``q_weight``, ``k_weight`` ``[head_dim]``
-    bf16: rows are normed with them first.  The tensors are kept, not copied: what is written into them later counts."""
+    bf16: rows are normed with them first.  The memory of the tensors is kept, not copied: what is written into it later
+    counts.  A tensor that is given other memory (a module's parameter, when the module is moved or cast) wants a new rotation."""
 
     def __init__(self, inv_freq: torch.Tensor, head_dim: int, *, axis: Optional[Sequence[int]] = None, adjacent: bool = False,
                  q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6):
@@ -62,6 +63,8 @@ class ApbvRotation:
         eps = float(eps)
         if not (eps >= 0.0 and math.isfinite(eps)):
             raise ValueError("eps: expected a finite number, not negative")
+        # (tensors of its own on that memory: theirs may be replaced, which would free what the addresses below name)
+        inv_freq, q_weight, k_weight = (None if t is None else t.detach() for t in (inv_freq, q_weight, k_weight))
         self.inv_freq, self.q_weight, self.k_weight, self.head_dim = inv_freq, q_weight, k_weight, head_dim
         self._made_of = (inv_freq, head_dim, axes, bool(adjacent), q_weight, k_weight, eps)
         self.n_axes, self.rot_dim, self.device = max(axes) + 1, 2 * pairs, inv_freq.device
