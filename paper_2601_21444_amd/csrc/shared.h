@@ -8,7 +8,7 @@ namespace apbv {
 struct SharedParams {
   CacheAttnParams prefix, own;       // the groups over their prefixes, the requests over their own keys
 };
-apbv_status launch_shared_short(const SharedParams& p, int head_dim, int waves, hipStream_t stream);      // shared_short.hip
+apbv_status launch_shared_short(const SharedParams& p, const SharedPlan& plan, int head_dim, hipStream_t stream);      // shared_short.hip
 apbv_status launch_shared_attention(const SharedParams& p, const SharedPlan& plan, int head_dim, hipStream_t stream);
 
 }  // namespace apbv

@@ -22,7 +22,7 @@ apbv_status apbv_cache_shared_attention(const apbv_cache* cache, int n_groups, i
   if (st != APBV_OK || q.tokens == 0) return st;
   const SharedPlan plan = choose_shared_plan(n_groups, n_requests, n_q_heads, n_kv_heads, head_dim, q.tokens, max_q,
                                              max_prefix_blocks * cache->page_size, max_blocks * cache->page_size,
-                                             group_starts == nullptr || n_groups == 1);
+                                             group_starts == nullptr && q_starts == nullptr);
   const SharedSpace space = shared_space(plan, n_groups, n_requests, q.tokens, n_q_heads, head_dim);
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < space.bytes) return APBV_ERR_WORKSPACE;
   char* const ws = static_cast<char*>(workspace);

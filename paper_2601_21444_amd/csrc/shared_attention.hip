@@ -308,7 +308,7 @@ apbv_status launch_dim(const SharedParams& p, const SharedPlan& plan, hipStream_
 }  // namespace
 
 apbv_status launch_shared_attention(const SharedParams& p, const SharedPlan& plan, int head_dim, hipStream_t stream) {
-  if (plan.whole) return launch_shared_short(p, head_dim, plan.short_waves, stream);
+  if (plan.whole) return launch_shared_short(p, plan, head_dim, stream);
   return head_dim == 128 ? launch_dim<128>(p, plan, stream) : launch_dim<64>(p, plan, stream);
 }
 

@@ -31,7 +31,13 @@ struct SharedPlan {
   int join_waves;            // waves that join the parts of a row: 1 or 4
   bool whole;                // a workgroup for every (group, KV head, 16 rows), with all their keys: prefix.row_tiles of a group
   int short_waves;           // waves of such a workgroup
+  int64_t slots;             // such workgroups for every KV head
 };
+
+// Where the host does not know how many rows each group has, its row tiles of 16 are found by slots: those of the e-th of all that may have
+// rows (the groups, and where they are listed the requests in front of them and behind) begin at this one, `query` being its first query.  It
+// has at most one slot more than row tiles: r rows behind a have ceil(r / 16) <= (a + r) / 16 - a / 16 + 1.
+constexpr int first_slot(int query, int group, int e) { return (int)((int64_t)query * group / 16) + e; }
 
 // Row tiles of 16 rows over the prefixes, though the rows would fill some of 32 or 128: a wave works on one by itself, from its start to
 // its part in 2 us and a little more for every tile; a row tile of 128 takes a workgroup 5 us longer to start and to end, but a fourth
@@ -74,10 +80,11 @@ inline int64_t parts_of_a_row(const CachePlan& p, int64_t units, int64_t tiles) 
 // Eight waves share the tiles, four where there are more such workgroups than units anyway (us, eight / four waves: 11 requests of 8 / 2 heads
 // of 64, 6, 15 6.8 / 8.0; 154 as above 21.3 / 22.4; 12 x 48 questions, 294, 94 28.8 / 34.5; 196 requests of 28 / 4,
 // 344, 46 36.2 / 33.4, 248, 436, 19 24.8 / 20.2).
-// Groups whose sizes only the device knows have no such workgroups of their own, and the largest keeps its few for long: 8 requests of 8 / 8 heads
-// of 128 behind 5 prefixes, 10 tiles on average, 13.3 / 7.3, 87 of 28 / 4 behind 2, 10 17.5 / 13.8, 33 of 16 / 2 behind 2, 11 13.9 / 14.8, 60 of 8 /
-// 8 behind 7, 18 13.5 / 24.2, 92 behind 4, 37 17.7 / 30.0.
-// max_prefix and max_len: keys that a row of the tables holds; even: groups are of equally many requests.
+// Groups whose sizes only the device knows are dealt by slots, so that the largest has as many workgroups as its rows need (us, cut / whole: 8
+// requests of 8 / 8 heads of 128 behind 5 prefixes of 333 keys 12.4 / 9.5, 87 of 28 / 4 behind 2 of 300, 57 behind one, 17.3 / 9.0, 33 of 16 / 2
+// behind 2 of 600 13.6 / 10.0, 60 of 8 / 8 behind 7 of 300 16.3 / 27.1, 92 behind 4 of 700 24.1 / 35.6; 4096 behind 1000 of 256, 3097 behind one,
+// 246 / 162, spread evenly 247 / 154).  The same limit holds for them: over fifty such calls, half of them taken whole, 1.003 of the faster form.
+// max_prefix and max_len: keys that a row of the tables holds; even: groups are of equally many requests, and these of equally many rows.
 inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q, int64_t max_prefix,
                                      int64_t max_len, bool even) {
   SharedPlan p;
@@ -107,8 +114,9 @@ inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int h
   const int64_t per_tile = (int64_t)n_requests * 16 / (n_rows * group) + 1, of_group = (n_requests + n_groups - 1) / n_groups;      // requests
   const int64_t tiles = prefix_tiles + (per_tile < of_group ? per_tile : of_group) * own_tiles;
   const int64_t more = row_tiles_16 > 48 ? (row_tiles_16 - 48) * 7 / 10 : 0, some = (d == 128 ? 24 : 32) + more;
-  const int64_t few = !even ? 10 : some < 80 ? some : 80;
-  p.whole = tiles <= few && row_tiles_16 + 2 * (int64_t)hkv * row_tiles <= (int64_t)1 << 22;
+  const int64_t few = some < 80 ? some : 80;
+  p.slots = even ? n_groups * row_tiles : n_rows * group / 16 + n_groups + 2;
+  p.whole = tiles <= few && row_tiles_16 + 2 * (int64_t)hkv * row_tiles <= (int64_t)1 << 22 && p.slots * hkv <= (int64_t)1 << 22;
   p.short_waves = row_tiles_16 <= 320 ? 8 : 4;
   if (p.whole) p.prefix.row_tiles = (int)row_tiles;
   return p;
