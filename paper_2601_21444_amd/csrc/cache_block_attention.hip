@@ -9,14 +9,15 @@
 // 32x32x16 and not beside 16x16x32.  Weights are rounded to bf16 for the product with V, as in all attention here
 // (cache_attention.hip).
 //
-// Chunks of prompts, two waves a SIMD, are bound by what a SIMD issues: matrix instructions are under way in 49 % of the cycles, vector
-// instructions (exponentials, conversions of keys and of weights, maxima) in 41 % more, and little of the one runs beside the other
-// (1020 TFLOP/s at 2.03 GHz; a kernel of 16x16x32 instructions, and one whose waves took K from memory each for itself, which convert
+// Chunks of prompts, two waves a SIMD, are bound by what a SIMD issues: matrix instructions are under way in 53 % of the cycles, vector
+// instructions (exponentials, conversions of keys and of weights, maxima) in 43 % more, and little of the one runs beside the other
+// (1030 TFLOP/s at 1.89 GHz; a kernel of 16x16x32 instructions, and one whose waves took K from memory each for itself, which convert
 // as much or more, run at the same rate to a percent: 4 x 512 queries of 28 / 4 heads of 128 over 20000 keys 568, 568, 574 us).
 // A turn of the loop is two tiles without a way out between them, holds the scales as bytes and keeps the maxima where they are written: else the
 // compiler waits for codes that have just been asked for, and forms the maxima behind the last matrix instruction (4 x 1 to 512 queries over
-// 9000 to 40000 keys 300.6 / 291.9 us).  Every row tile of a head converts its keys again.  Short blocks are bound by their start (4 us), the end (3 us) and 3000 cycles a
-// tile of a lone wave, of which 1024 are matrix instructions.
+// 9000 to 40000 keys 292.8 / 282.6 us, both in one run).  Every row tile of a head converts its keys again.  Short blocks are bound by their start
+// (4 us), the end (3 us) and 3000 cycles a tile of a lone wave, of which 1024 are matrix instructions.  At head_dim 128 19 registers are spilled
+// (25 with lse), where a piece begins and ends, none in the loop.
 #include "cache_block_rows.h"
 
 namespace apbv {

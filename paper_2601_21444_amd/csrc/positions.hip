@@ -12,8 +12,8 @@
 // fast as float32 does here): codes are those of the exact value, whatever the order of the arithmetic.  The 21 leading bits and a
 // bit for all that lie behind them are what a float32 is given, which rounds to the same code.
 //
-// Bound.  Rows that go to bf16, by HBM: 16384 tokens of 16 + 2 heads of 128 (151 MB) 25.4 us, 5.9 TB/s; 32768 of 28 + 4, normed (537 MB)
-// 91 us, 5.9 TB/s; a copy of 1 GiB reaches 5.2.  Few tokens by the launch and a chain of position, angle, row: 2.5 us.  Rows that are bound for the
+// Bound.  Rows that go to bf16, by HBM: 16384 tokens of 16 + 2 heads of 128 (151 MB) 25.9 us, 5.8 TB/s; 32768 of 28 + 4, normed (537 MB)
+// 93 us, 5.8 TB/s; a copy of 1 GiB reaches 5.2.  Few tokens by the launch and a chain of position, angle, row: 2.5 us.  Rows that are bound for the
 // cache by float64 arithmetic: keys and values of 16384 tokens of 2 heads of 128 12.2 us, where cache_store_kernel takes 5.6; with 16 heads of
 // queries beside them 34.8 (157 MB, 4.5 TB/s).  Loads that pass the caches by 28.6 / 25.2 us and 94.3 / 96.6 (with / without, of the first two);
 // five waves a SIMD 43.5 / 35.1 (the third); workgroups of keys among those of the queries 37.8 / 36.2.

@@ -6,13 +6,18 @@
 // axis, are left in float32 and joined by a second launch.
 //
 // Bound, behind long prefixes, by what a SIMD issues (cache_block_attention.hip): 64 questions of 16 / 2 heads of 128 behind 133120 keys
-// take 89 us, of which the first launch is 80 (70 GFLOP, 880 TFLOP/s: matrix instructions under way in 42 % of the cycles, vector
-// instructions in 37 % more, little of the one beside the other) and the second, which reads 34 MB of parts, 9; the same 64 rows as one
-// request of apbv_cache_attention, without own keys, take 88.  256 requests of 28 / 4 heads behind 32768 keys, 65 to 2048 of their own
-// 153 (122 GFLOP and 75 MB of own keys), as one request without them 132.  Tried and not kept (us, so / then): waves of 64 rows, one a SIMD
+// take 90 us from a graph.  In a trace, which times each launch from its own start, the first is 84 (70 GFLOP, 835 TFLOP/s: matrix instructions
+// under way in 42 % of the cycles, vector instructions in 37 % more, little of the one beside the other) and the second, which reads 34 MB of
+// parts, 10; the same 64 rows as one request of apbv_cache_attention, without own keys, take 88.  256 requests of 28 / 4 heads behind 32768 keys,
+// 65 to 2048 of their own 152 to 156 (122 GFLOP and 75 MB of own keys), as one request without them 132.  One launch holds two bodies, and at head_dim
+// 128 the compiler spills 26 to 40 registers in the instances with row tiles of 32 or 128, where a piece begins and ends, none in the loop over
+// tiles: 14 MB written beside the parts of the first call.  Tried and not kept (us, so / then): waves of 64 rows, one a SIMD
 // with 512 registers, which read half of the LDS bytes, 90 / 99 and 136 / 144 (a lone wave's matrix and vector instructions do not
 // overlap either, and 90 moves between the register files come with every 32 keys); workgroups for the one axis or the other by
 // what they cost 205 / 238 (300 requests behind 40000 keys, up to 300 of their own); parts in the order in which lanes store them, 90.4 / 92.1.
+//
+// Weights are rounded to bf16 for the product with V (cache_attention.hip): outputs lie 1.9 to 2.4e-3 from those of 64 bits, root mean square,
+// where float32 weights leave 1.5 to 1.7e-3, the rounding of the output alone.
 //
 // Behind shorter prefixes it is bound by its start, the end of the longest share and the join, 12 us with row tiles of 16 rows (shared_validation.h).
 #include "cache_block_rows.h"

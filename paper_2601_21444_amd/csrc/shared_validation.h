@@ -29,7 +29,7 @@ struct SharedPlan {
   CachePlan prefix, own;
   size_t prefix_parts, own_parts;      // bytes of the workspace, whatever the tables hold
   int join_waves;            // waves that join the parts of a row: 1 or 4
-  bool whole;                // a workgroup for every (group, KV head, 16 rows), with all their keys: prefix.row_tiles of a group
+  bool whole;                // a workgroup for every (group, KV head, 16 rows), with all their keys: prefix.row_tiles of a group where all are alike
   int short_waves;           // waves of such a workgroup
   int64_t slots;             // such workgroups for every KV head
 };
@@ -52,6 +52,8 @@ constexpr int first_slot(int query, int group, int e) { return (int)((int64_t)qu
 // Of 32 / of 16: 17 requests of 8 / 8 heads of 128 behind 3598 18.2 / 14.1 (tiles_16 912), 88 behind 4 of 4933 25.8 / 20.3 (4992), 74
 // behind 3 of 20066 43.7 / 40.3 (15072), 4 of 28 / 4 behind 160000 39.0 / 41.5 (20000); 64: 6 of 8 / 2 behind 2293 12.8 / 11.9 (144), 96 of 2 / 1
 // behind 8 of 19798 19.3 / 18.2 (4960), 48 of 8 / 2 behind 7 of 1500 to 16384 18.0 / 19.3 (7196).
+// A line between these points, too; of those listed it takes the slower height for 16 requests behind 34286 keys (30.3 for 28.7) and 11 behind 67889
+// (31.6 for 28.6).
 inline bool low_row_tiles(int d, bool high, int64_t tiles_16, int64_t tiles) {
   if (!high) return tiles_16 <= (d == 128 ? 16000 : 5000);
   return tiles_16 <= (d == 128 ? 6000 + tiles * 7 / 2 : 1500 + tiles * 3);
@@ -73,13 +75,15 @@ inline int64_t parts_of_a_row(const CachePlan& p, int64_t units, int64_t tiles) 
 
 // Where the tables hold but a few tiles, a workgroup takes 16 rows and all the keys that they see, without a second launch: 5 us and
 // 0.25 for every tile, where a cut call takes 12 and more.  How many tiles are few depends on how many such workgroups there are to even them
-// out (us, cut / whole; number of row tiles of 16, tiles of the prefix and of the own keys that one sees): 4 requests of 8 / 2 heads of 64,
-// 2, 22 12.4 / 10.5; 8, 4, 48 12.2 / 12.6; 44, 22, 42 13.4 / 10.7; 4 of 8 / 8 of 128, 8, 31 13.5 / 13.3; 7, 8, 33 12.7 / 16.9; 3 x 54 questions,
-// 48, 38 15.7 / 19.8, 10 x 22, 64, 33 17.3 / 17.9; 191 requests, 96, 69 26.9 / 25.2; 65 of 28 / 4, 116, 70 28.3 / 22.2; 10 x 27 questions of 8 /
-// 8, 72, 83 21.8 / 33.5; 154 requests of 16 / 2, 154, 54 30.8 / 21.3; 94 of 28 / 4, 168, 101 33.6 / 35.1, 5 x 46 questions, 208, 34 25.6 / 15.6.
+// out (us, cut / whole; number of row tiles of 16, tiles of the prefix and of the own keys that one sees).  Heads of 64: 11 requests of 8 / 2, 6, 15
+// 12.0 / 7.7; 4, 2, 22 11.7 / 9.5; 8, 4, 48 12.3 / 13.4; 10 x 22 questions, 110, 29 17.8 / 11.8; 114 requests of 2 / 1, 15, 53 14.6 / 15.6.  Heads of 128:
+// 4 of 8 / 8, 8, 31 13.2 / 14.1; 7, 8, 33 13.0 / 16.3; 60 behind 7 prefixes, 56, 41 16.6 / 19.0; 191, 96, 69 27.0 / 29.4; 154 of 16 / 2, 154, 54 25.5 /
+// 20.9; 3 x 54 questions, 162, 38 24.5 / 16.4; 94 of 28 / 4, 168, 99 37.3 / 39.2; 256, 448, 19 35.9 / 17.0; 5 x 46 questions, 404, 34 41.9 / 27.9.
+// It is a line between such points, and near it the slower form is taken: 83 requests of 8 / 2 heads of 64, 42, 33 cut, 14.6 / 11.1; 44, 22, 42 cut,
+// 13.1 / 12.5; 65 of 28 / 4 of 128, 116, 70 whole, 25.0 / 29.3; 10 x 27 questions of 8 / 8, 136, 82 cut, 32.8 / 31.4.
 // Eight waves share the tiles, four where there are more such workgroups than units anyway (us, eight / four waves: 11 requests of 8 / 2 heads
-// of 64, 6, 15 6.8 / 8.0; 154 as above 21.3 / 22.4; 12 x 48 questions, 294, 94 28.8 / 34.5; 196 requests of 28 / 4,
-// 344, 46 36.2 / 33.4, 248, 436, 19 24.8 / 20.2).
+// of 64, 6, 15 7.7 / 9.1; 154 as above 20.9 / 25.3; 196 requests of 28 / 4, 344, 46 41.3 / 38.1; 248, 436, 19 24.8 / 20.6; 12 x 48 questions, 1008,
+// 87 103 / 87.8).
 // Groups whose sizes only the device knows are dealt by slots, so that the largest has as many workgroups as its rows need (us, cut / whole: 8
 // requests of 8 / 8 heads of 128 behind 5 prefixes of 333 keys 12.4 / 9.5, 87 of 28 / 4 behind 2 of 300, 57 behind one, 17.3 / 9.0, 33 of 16 / 2
 // behind 2 of 600 13.6 / 10.0, 60 of 8 / 8 behind 7 of 300 16.3 / 27.1, 92 behind 4 of 700 24.1 / 35.6; 4096 behind 1000 of 256, 3097 behind one,
