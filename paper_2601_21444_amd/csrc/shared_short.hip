@@ -9,8 +9,10 @@
 // rule when it is taken, and how many waves there are, stands in shared_validation.h.
 //
 // No workgroup has more than one row tile, and none walks over requests that are not near its rows: both are found by a search 64 ways over the
-// starts, twice where there are more than 64 (us, with a loop over row tiles, as many workgroups for every group as the average needs, and over
-// requests / so: 4096 requests of 8 / 8 heads of 128 behind 1000 prefixes of 256 keys, 3097 of them behind one, 5134 / 162, 4096 behind one 174 / 73).
+// starts, twice where there are more than 62 groups (us, with a loop over row tiles, as many workgroups for every group as the average needs, and
+// over requests / so: 4096 requests of 8 / 8 heads of 128 behind 1000 prefixes of 256 keys, 3097 of them behind one, 5124 / 149, 4096 behind one 174 / 70;
+// 4096 behind as many prefixes of 64 keys, ten of them with a row, 45.5 / 6.6).  The search costs a small call 0.3 us, one of 64 groups of one
+// request 0.9 (6.1 / 7.0).
 #include "cache_few_rows.h"
 #include "shared.h"
 
@@ -57,30 +59,29 @@ __global__ __launch_bounds__(64 * W, 2) void shared_short_kernel(const SharedPar
     first = start_of(from);
     past = start_of(to);
   } else {
-    // the last that begins at or before the slot: a wave's lanes look at 64 of them, or at every step-th
+    // the last that begins at or before the slot.  A wave's lanes look at where 64 of them begin, or every step-th; the last entry is where all end
     const int n = p.prefix.n_requests + (listed ? 2 : 0);
-    int e = 0, top = n, step = (n + 63) / 64, begin;
+    int e = 0, top = n, step = (n + 64) / 64, begin;
 #pragma unroll 1
     for (;;) {
-      const int x = e + lane * step < top ? e + lane * step : top - 1;
-      const int b0 = !listed ? x * p.prefix.members_each : x == 0 ? 0 : clip(p.prefix.members[x - 1], own.n_requests);
-      const int b1 = !listed ? b0 + p.prefix.members_each : x == n - 1 ? own.n_requests : clip(p.prefix.members[x], own.n_requests);
-      const int q0 = clip(own.starts ? own.starts[b0] : b0 * own.each, own.n_rows), q1 = clip(own.starts ? own.starts[b1] : b1 * own.each, own.n_rows);
-      const int its_begin = first_slot(q0, own.group, x);
+      const int x = e + lane * step < top ? e + lane * step : top;
+      const int b = !listed ? x * p.prefix.members_each : x == 0 ? 0 : x == n ? own.n_requests : clip(p.prefix.members[x - 1], own.n_requests);
+      const int q = clip(own.starts ? own.starts[b] : b * own.each, own.n_rows);
+      const int its_begin = first_slot(q, own.group, x);
       const uint64_t before = __builtin_amdgcn_ballot_w64(e + lane * step < top && its_begin <= slot);
       if (before == 0) return;
       const int at = 63 - __builtin_clzll(before);
       e += at * step;
       if (step == 1) {
-        from = __builtin_amdgcn_readlane(b0, at);
-        to = __builtin_amdgcn_readlane(b1, at);
-        first = __builtin_amdgcn_readlane(q0, at);
-        past = __builtin_amdgcn_readlane(q1, at);
+        from = __builtin_amdgcn_readlane(b, at);
+        to = __builtin_amdgcn_readlane(b, at + 1);
+        first = __builtin_amdgcn_readlane(q, at);
+        past = __builtin_amdgcn_readlane(q, at + 1);
         begin = __builtin_amdgcn_readlane(its_begin, at);
         break;
       }
       top = e + step < n ? e + step : n;
-      step = (step + 63) / 64;
+      step = (step + 64) / 64;
     }
     rt = slot - begin;
     g = listed ? e - 1 : e;
@@ -286,12 +287,20 @@ __global__ __launch_bounds__(64 * W, 2) void shared_short_kernel(const SharedPar
             l_run = __builtin_amdgcn_fdot2_f32_bf16(c, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l_run, false);
             pw[2 * mb + (e >> 1)] = __builtin_bit_cast(uint32_t, c);
           }
-#pragma unroll
-        for (int d = 0; d < T::DBN; ++d) {
+        // (two reads ahead of the matrix instruction, and kept there: left to itself the compiler waits for each by itself where it has registers to save
+        // for a third wave of a SIMD, 16 requests of 8 / 8 heads of 128 behind 192 keys, 64 of their own, 13.0 / 12.3 us)
+        auto of_v = [&](int d) {
           const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((APBV_LDS(s16x4))(vbuf + v_off[d]));
           const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((APBV_LDS(s16x4))(vbuf + 16 * T::ROW_BYTES + v_off[d]));
-          const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, pw), o[d], 0, 0, 0);
+          return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        bf16x8 a[2] = {of_v(0), of_v(1)};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int d = 0; d < T::DBN; ++d) {
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[d % 2], __builtin_bit_cast(bf16x8, pw), o[d], 0, 0, 0);
+          if (d + 2 < T::DBN) a[d % 2] = of_v(d + 2);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
       load_v();

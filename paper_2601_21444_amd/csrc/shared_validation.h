@@ -36,8 +36,8 @@ struct SharedPlan {
 
 // Where the host does not know how many rows each group has, its row tiles of 16 are found by slots: those of the e-th of all that may have
 // rows (the groups, and where they are listed the requests in front of them and behind) begin at this one, `query` being its first query.  It
-// has at most one slot more than row tiles: r rows behind a have ceil(r / 16) <= (a + r) / 16 - a / 16 + 1.
-constexpr int first_slot(int query, int group, int e) { return (int)((int64_t)query * group / 16) + e; }
+// has at most one slot more than row tiles, as r rows behind a have ceil(r / 16) <= (a + r) / 16 - a / 16 + 1; one without rows need not have any.
+constexpr int first_slot(int query, int group, int e) { return (int)((int64_t)query * group / 16) + (e < query ? e : query); }
 
 // Row tiles of 16 rows over the prefixes, though the rows would fill some of 32 or 128: a wave works on one by itself, from its start to
 // its part in 2 us and a little more for every tile; a row tile of 128 takes a workgroup 5 us longer to start and to end, but a fourth
@@ -76,18 +76,20 @@ inline int64_t parts_of_a_row(const CachePlan& p, int64_t units, int64_t tiles) 
 // Where the tables hold but a few tiles, a workgroup takes 16 rows and all the keys that they see, without a second launch: 5 us and
 // 0.25 for every tile, where a cut call takes 12 and more.  How many tiles are few depends on how many such workgroups there are to even them
 // out (us, cut / whole; number of row tiles of 16, tiles of the prefix and of the own keys that one sees).  Heads of 64: 11 requests of 8 / 2, 6, 15
-// 12.0 / 7.7; 4, 2, 22 11.7 / 9.5; 8, 4, 48 12.3 / 13.4; 10 x 22 questions, 110, 29 17.8 / 11.8; 114 requests of 2 / 1, 15, 53 14.6 / 15.6.  Heads of 128:
-// 4 of 8 / 8, 8, 31 13.2 / 14.1; 7, 8, 33 13.0 / 16.3; 60 behind 7 prefixes, 56, 41 16.6 / 19.0; 191, 96, 69 27.0 / 29.4; 154 of 16 / 2, 154, 54 25.5 /
-// 20.9; 3 x 54 questions, 162, 38 24.5 / 16.4; 94 of 28 / 4, 168, 99 37.3 / 39.2; 256, 448, 19 35.9 / 17.0; 5 x 46 questions, 404, 34 41.9 / 27.9.
-// It is a line between such points, and near it the slower form is taken: 83 requests of 8 / 2 heads of 64, 42, 33 cut, 14.6 / 11.1; 44, 22, 42 cut,
-// 13.1 / 12.5; 65 of 28 / 4 of 128, 116, 70 whole, 25.0 / 29.3; 10 x 27 questions of 8 / 8, 136, 82 cut, 32.8 / 31.4.
+// 11.9 / 7.7; 4, 2, 22 11.7 / 9.5; 8, 4, 48 12.3 / 13.5; 10 x 22 questions, 110, 29 17.6 / 11.8; 114 requests of 2 / 1, 15, 53 14.6 / 15.6.  Heads of 128:
+// 7 of 8 / 8, 8, 33 13.0 / 15.1; 60 behind 7 prefixes, 56, 41 16.3 / 17.7; 191, 96, 69 27.0 / 27.2; 154 of 16 / 2, 154, 54 25.1 / 19.0; 3 x 54
+// questions, 162, 38 24.4 / 15.2; 256 requests of 28 / 4, 448, 19 35.9 / 15.9; 5 x 46 questions, 404, 34 42.0 / 24.4.
+// It is a line between such points, and near it the slower form is taken: 83 requests of 8 / 2 heads of 64, 42, 33 cut, 14.5 / 11.1; 44, 22, 42 cut,
+// 13.1 / 12.5; 65 of 28 / 4 of 128, 116, 70 whole, 25.2 / 26.2; 94, 168, 99 cut, 36.4 / 35.8; 10 x 27 questions of 8 / 8, 136, 82 cut, 32.7 / 28.5; 12 x 48
+// of 28 / 4, 1008, 87 cut, 86.9 / 82.3.
 // Eight waves share the tiles, four where there are more such workgroups than units anyway (us, eight / four waves: 11 requests of 8 / 2 heads
-// of 64, 6, 15 7.7 / 9.1; 154 as above 20.9 / 25.3; 196 requests of 28 / 4, 344, 46 41.3 / 38.1; 248, 436, 19 24.8 / 20.6; 12 x 48 questions, 1008,
-// 87 103 / 87.8).
+// of 64, 6, 15 7.7 / 9.1; 154 as above 19.5 / 22.6; 196 requests of 28 / 4, 344, 46 38.3 / 35.1; 248, 436, 19 23.1 / 19.2; 12 x 48 questions, 1008,
+// 87 93.6 / 82.3).
 // Groups whose sizes only the device knows are dealt by slots, so that the largest has as many workgroups as its rows need (us, cut / whole: 8
-// requests of 8 / 8 heads of 128 behind 5 prefixes of 333 keys 12.4 / 9.5, 87 of 28 / 4 behind 2 of 300, 57 behind one, 17.3 / 9.0, 33 of 16 / 2
-// behind 2 of 600 13.6 / 10.0, 60 of 8 / 8 behind 7 of 300 16.3 / 27.1, 92 behind 4 of 700 24.1 / 35.6; 4096 behind 1000 of 256, 3097 behind one,
-// 246 / 162, spread evenly 247 / 154).  The same limit holds for them: over fifty such calls, half of them taken whole, 1.003 of the faster form.
+// requests of 8 / 8 heads of 128 behind 5 prefixes of 333 keys 12.4 / 8.9, 87 of 28 / 4 behind 2 of 300, 57 behind one, 16.7 / 8.3, 33 of 16 / 2
+// behind 2 of 600 13.4 / 9.4, 60 of 8 / 8 behind 7 of 300 16.4 / 24.9, 92 behind 4 of 700 23.9 / 32.9; 4096 behind 1000 of 256, 3097 behind one,
+// 246 / 149, spread evenly 247 / 142).  The same limit holds for them: over fifty such calls the form taken is as fast as the faster one, but for one
+// (83 requests of 8 / 2 heads of 64, as above).
 // max_prefix and max_len: keys that a row of the tables holds; even: groups are of equally many requests, and these of equally many rows.
 inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int hkv, int d, int64_t n_rows, int64_t max_q, int64_t max_prefix,
                                      int64_t max_len, bool even) {
@@ -119,7 +121,7 @@ inline SharedPlan choose_shared_plan(int n_groups, int n_requests, int hq, int h
   const int64_t tiles = prefix_tiles + (per_tile < of_group ? per_tile : of_group) * own_tiles;
   const int64_t more = row_tiles_16 > 48 ? (row_tiles_16 - 48) * 7 / 10 : 0, some = (d == 128 ? 24 : 32) + more;
   const int64_t few = some < 80 ? some : 80;
-  p.slots = even ? n_groups * row_tiles : n_rows * group / 16 + n_groups + 2;
+  p.slots = even ? n_groups * row_tiles : n_rows * group / 16 + (n_groups + 2 < n_rows ? n_groups + 2 : n_rows);
   p.whole = tiles <= few && row_tiles_16 + 2 * (int64_t)hkv * row_tiles <= (int64_t)1 << 22 && p.slots * hkv <= (int64_t)1 << 22;
   p.short_waves = row_tiles_16 <= 320 ? 8 : 4;
   if (p.whole) p.prefix.row_tiles = (int)row_tiles;

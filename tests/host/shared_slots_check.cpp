@@ -30,27 +30,26 @@ struct Found {
 // shared_short.hip, lane after lane; `at` checks every index.
 static bool find(const Call& c, int slot, Found& f) {
   const int n = c.n_groups + (c.members ? 2 : 0);
-  int e = 0, top = n, step = (n + 63) / 64, rounds = 0;
+  int e = 0, top = n, step = (n + 64) / 64, rounds = 0;
   for (;;) {
     CHECK(++rounds <= 3);
-    int last = -1, b0[64], b1[64], q0[64], q1[64], begin[64];
+    int last = -1, b[64], q[64], begin[64];
     for (int lane = 0; lane < 64; ++lane) {
-      const int x = e + lane * step < top ? e + lane * step : top - 1;
-      b0[lane] = !c.members ? x * c.members_each : x == 0 ? 0 : clip(c.members->at(x - 1), c.n_requests);
-      b1[lane] = !c.members ? b0[lane] + c.members_each : x == n - 1 ? c.n_requests : clip(c.members->at(x), c.n_requests);
-      q0[lane] = c.row_of(b0[lane]);
-      q1[lane] = c.row_of(b1[lane]);
-      begin[lane] = first_slot(q0[lane], c.group, x);
+      const int x = e + lane * step < top ? e + lane * step : top;
+      b[lane] = !c.members ? x * c.members_each : x == 0 ? 0 : x == n ? c.n_requests : clip(c.members->at(x - 1), c.n_requests);
+      q[lane] = c.row_of(b[lane]);
+      begin[lane] = first_slot(q[lane], c.group, x);
       if (e + lane * step < top && begin[lane] <= slot) last = lane;
     }
     if (last < 0) return false;
     e += last * step;
     if (step == 1) {
-      f = Found{c.members ? e - 1 : e, slot - begin[last], b0[last], b1[last], q0[last], q1[last]};
+      CHECK(last < 63);
+      f = Found{c.members ? e - 1 : e, slot - begin[last], b[last], b[last + 1], q[last], q[last + 1]};
       return true;
     }
     top = e + step < n ? e + step : n;
-    step = (step + 63) / 64;
+    step = (step + 64) / 64;
   }
 }
 
@@ -61,7 +60,7 @@ static void replay(int n_groups, int n_requests, int group, bool listed, bool ra
   std::vector<int32_t> starts(n_requests + 1), members(n_groups + 1);
   const int lead = ragged ? below(20) : 0, each = 1 + below(3);
   starts[0] = lead;
-  for (int b = 0; b < n_requests; ++b) starts[b + 1] = starts[b] + (shape == 1 ? below(2) : shape == 2 ? (b == n_requests / 2 ? 500 : 1) : below(4));
+  for (int b = 0; b < n_requests; ++b) starts[b + 1] = starts[b] + (shape == 1 ? below(2) : shape == 4 ? (below(40) ? 0 : below(3)) : shape == 2 ? (b == n_requests / 2 ? 500 : 1) : below(4));
   for (int& m : members) m = below(n_requests + 1);
   std::sort(members.begin(), members.end());
   if (shape == 3)                                      // one group has nearly all
@@ -78,7 +77,7 @@ static void replay(int n_groups, int n_requests, int group, bool listed, bool ra
   c.starts = ragged ? &starts : nullptr;
   if (c.n_rows == 0) return;
   const SharedPlan p = choose_shared_plan(n_groups, n_requests, 2 * group, 2, 64, c.n_rows, 4, 64, 64, false);
-  CHECK(p.slots <= (int64_t)c.n_rows * group / 16 + n_groups + 2);
+  CHECK(p.slots <= (int64_t)c.n_rows * group / 16 + std::min(n_groups + 2, c.n_rows));
   // rows of every group, and of those in front and behind, each to be taken once
   std::vector<int> taken(c.n_rows * group, 0);
   int idle = 0;
@@ -111,7 +110,7 @@ int main() {
   for (int n_groups : {1, 2, 3, 61, 62, 63, 64, 65, 130, 1000, 4094, 4095, 4096})
     for (int times : {1, 2, 5})
       for (int group : {1, 2, 7, 8, 33})
-        for (int shape = 0; shape < 4; ++shape) {
+        for (int shape = 0; shape < 5; ++shape) {
           const int n_requests = n_groups * times;
           if (n_requests > 4096 || (n_groups >= 1000 && group > 2)) continue;
           replay(n_groups, n_requests, group, true, true, shape);
@@ -126,7 +125,7 @@ int main() {
     for (int& x : members) x = (int32_t)rng();
     const Call c = {n_groups, n_requests, 3, 1000, 1, 1, &members, &starts};
     Found f;
-    for (int slot = 0; slot < 1000 * 3 / 16 + n_groups + 2; ++slot)
+    for (int slot = 0; slot < 1000 * 3 / 16 + n_groups + 2; ++slot)      // (more than there are)
       if (find(c, slot, f)) CHECK(f.rt >= 0 && f.from >= 0 && f.from <= n_requests && f.first >= 0 && f.first <= 1000 && f.past <= 1000);
   }
   // the launch: never more workgroups than 2^22, and of groups of unknown sizes no fewer than their row tiles may be
@@ -140,7 +139,7 @@ int main() {
               const SharedPlan p = choose_shared_plan(n_groups, n_requests, hkv * group, hkv, 128, rows, 1, 64, 64, even);
               if (!p.whole) continue;
               CHECK(p.slots >= 1 && p.slots * hkv <= 1 << 22);
-              CHECK(even ? p.slots == (int64_t)n_groups * p.prefix.row_tiles : p.slots * 16 >= rows * group + 16 * n_groups);
+              CHECK(even ? p.slots == (int64_t)n_groups * p.prefix.row_tiles : p.slots * 16 > rows * group && p.slots <= rows * group / 16 + rows);
             }
           }
   printf("slot checks OK\n");
